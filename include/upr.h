@@ -398,6 +398,188 @@ upr_status upr_mx_linear(const uint8_t* a_codes, const uint8_t* a_scales, const 
                          const uint8_t* w_scales, const float* bias, int64_t M, int32_t N,
                          int32_t K, float* out, void* stream);
 
+/* ---------------------------------------------------------------------
+ * Paged K/V cache: histories that grow.  A history encoded by
+ * upr_encode_user occupies one contiguous row range for good; here each
+ * user's rows live in pages of a common pool, so that a user's next actions
+ * are appended (upr_extend_user) instead of the history being encoded again.
+ * The operators that the paged model calls are made of are offered on their
+ * own: rotary positions, the append, and the attention over the pages.
+ *
+ * Pool layout: [planes][n_pages][2][n_kv_heads][page_rows][head_dim], a K
+ * block then a V block per page, heads outermost inside a block; one plane
+ * for the operators, n_layers planes for the model calls.  `tables` maps
+ * rows to pages: position p of user u is row p % page_rows of page
+ * tables[u * table_stride + p / page_rows].  A page may appear in several
+ * users' tables (a common prefix) as long as nothing is appended to it.
+ * Table entries are read by the kernels only (they may change between calls
+ * in stream order); an entry outside [0, n_pages) stands for a page whose
+ * rows read as zeros and to which nothing is written.
+ *
+ * Conventions of the paged calls, beyond those above:
+ *   - Segments are taken from offsets_host alone; offsets_dev is not read
+ *     and may be NULL.  rows_host[u] is the number of rows user u's cache
+ *     holds, the appended ones included: the new rows of user u take the
+ *     positions rows_host[u] - count_u .. rows_host[u] - 1.  Both arrays are
+ *     read during the call (a captured call replays the same lengths).
+ *     Users without new rows are skipped.
+ *   - UPR_ERR_OFFSETS: rows_host[u] negative or below count_u where the new
+ *     rows are part of it; UPR_ERR_CAPACITY: the table has fewer than
+ *     ceil(rows_host[u] / page_rows) entries per user; UPR_ERR_LIMIT:
+ *     page_rows not a power of two in [16, 1024], rows_host[u] above 2^30,
+ *     a leading dimension too small, or a buffer or leading dimension that is
+ *     not a multiple of 16 bytes; UPR_ERR_CONFIG: an unsupported shape.
+ *   - Leading dimensions (`_ld`) count elements between consecutive rows; a
+ *     row holds its heads one after the other.  Row r of a buffer is the
+ *     row r of the segments (offsets_host[0] > 0: a sub-range).
+ * --------------------------------------------------------------------- */
+typedef struct {
+    void* data;             /* device, 16-byte aligned                      */
+    int64_t n_pages;        /* pages per plane, below 2^31                  */
+    int32_t page_rows;      /* rows per page                                */
+    int32_t table_stride;   /* table entries per user                       */
+    const int32_t* tables;  /* device, [num_users][table_stride]            */
+} upr_paged_cache;
+
+/* Heads of the paged operators: dtype UPR_F32 or UPR_BF16 (queries, keys,
+ * values, outputs and cache), head_dim 32, 64 or 128, 1 <= n_kv_heads <=
+ * n_heads <= 1024, n_heads a multiple of n_kv_heads: query head h reads
+ * key/value head h / (n_heads / n_kv_heads). */
+typedef struct {
+    int32_t dtype;
+    int32_t n_heads;
+    int32_t n_kv_heads;
+    int32_t head_dim;
+} upr_attn_shape;
+
+/* Bytes of a pool for the model calls (0 if cfg is invalid, n_pages < 0 or
+ * page_rows is not allowed). */
+size_t upr_paged_cache_bytes(const upr_config* cfg, int64_t n_pages, int32_t page_rows);
+
+/* ---- Rotary positions.  Pair i of a head's first rot_dim features, at
+ * position p, is turned by the angle p * freq[i]:
+ *   a' = magnitude (a cos - b sin),   b' = magnitude (b cos + a sin).
+ * UPR_ROPE_HALF pairs features i and i + rot_dim / 2, UPR_ROPE_INTERLEAVED
+ * features 2i and 2i + 1; features past rot_dim are left as they are.
+ * Angles are formed and reduced in 64 bits, so far positions keep theirs;
+ * sines, cosines and products are fp32, rounded once to the storage type. */
+typedef enum { UPR_ROPE_HALF = 0, UPR_ROPE_INTERLEAVED = 1 } upr_rope_layout;
+
+/* Frequencies: freq[i] = base^(-2i / rot_dim), and for longer contexts
+ *   LINEAR:   freq[i] / factor
+ *   NTK:      with base * factor^(rot_dim / (rot_dim - 2)) (rot_dim >= 4)
+ *   BY_PARTS: pairs that make at most one turn over original_length are
+ *             divided by factor, those of 32 turns or more kept, the ones
+ *             between blended linearly in their turns; magnitude
+ *             1 + 0.1 ln(factor). */
+typedef enum {
+    UPR_ROPE_PLAIN = 0, UPR_ROPE_LINEAR = 1, UPR_ROPE_NTK = 2, UPR_ROPE_BY_PARTS = 3
+} upr_rope_scaling;
+
+#define UPR_ROPE_MAX_PAIRS 64
+
+typedef struct {
+    int32_t rot_dim;        /* even, 2 .. 2 * UPR_ROPE_MAX_PAIRS            */
+    int32_t layout;         /* a upr_rope_layout value                      */
+    double magnitude;
+    double freq[UPR_ROPE_MAX_PAIRS];    /* radians per position             */
+} upr_rope;
+
+/* Fills *out (host).  base > 1, factor >= 1, and for BY_PARTS
+ * original_length > 0 (UPR_ERR_LIMIT otherwise; factor and original_length
+ * are ignored where the scaling has none).  A caller may also fill the
+ * struct itself with finite values. */
+upr_status upr_rope_init(int32_t rot_dim, int32_t layout, double base, int32_t scaling, double factor,
+                         double original_length, upr_rope* out);
+
+/* out = x rotated, row r at positions[r] (device int32, any value): x and
+ * out [rows][heads][head_dim] of dtype UPR_F32 or UPR_BF16, head_dim 32, 64 or
+ * 128 and at least rot_dim, 1 <= heads <= 2048.  out may be x (same leading
+ * dimension); otherwise they must not overlap.  Allocates nothing. */
+upr_status upr_rope_apply(const upr_rope* rope, int32_t dtype, int32_t heads, int32_t head_dim, const void* x,
+                          int64_t x_ld, const int32_t* positions, int64_t rows, void* out, int64_t out_ld,
+                          void* stream);
+
+/* Writes the keys k and values v of the new rows into the pages, the keys
+ * rotated at their positions when rope is given (NULL: as they are).  With q,
+ * the queries of the same rows go to q_out likewise (rotated, or copied
+ * without rope; q_out may be q with the same leading dimension); q and q_out
+ * are both NULL or both given.  Only the new rows' places in the pages are
+ * written; two new rows of one call must not share a place.  Allocates nothing. */
+upr_status upr_paged_append(const upr_attn_shape* shape, const upr_paged_cache* cache, const upr_segments* fresh,
+                            const int32_t* rows_host, const upr_rope* rope, const void* k, int64_t k_ld,
+                            const void* v, int64_t v_ld, const void* q, int64_t q_ld, void* q_out,
+                            int64_t q_out_ld, void* stream);
+
+/* How scores become weights: z = scale * q.k; softcap > 0: softcap *
+ * tanh(z / softcap); slopes (device float [n_heads], or NULL): plus
+ * slopes[h] * (key position - query position); then the softmax over the
+ * keys that the query sees. */
+typedef struct {
+    float scale;            /* > 0, below 1e30                              */
+    float softcap;          /* 0: none, or > 0, below 1e30, with a finite
+                             * scale / softcap                              */
+    int32_t window;         /* > 0: only the last `window` positions up to
+                             * the query's own, itself included; 0: all     */
+    const float* slopes;
+    /* NULL: the query rows are the cache's last rows of their user, and see
+     * positions up to their own.  Both given: the query rows are not in the
+     * cache (candidates); each stands at position rows_host[u], sees all
+     * cached rows of its user and its own key and value, row r of k_self and
+     * v_self [rows][n_kv_heads][head_dim], and no other candidate's. */
+    const void* k_self;
+    const void* v_self;
+    int64_t self_ld;        /* of both                                      */
+} upr_attn_options;
+
+/* Workspace bytes needed by upr_paged_attention (0 for none, or on invalid
+ * input).  Pointers inside options and the cache's pointers are not read. */
+size_t upr_paged_attention_workspace_bytes(const upr_attn_shape* shape, const upr_paged_cache* cache,
+                                           const upr_segments* queries, const int32_t* rows_host,
+                                           const upr_attn_options* options);
+
+/* Attention of the query rows q over their users' cached rows -> out
+ * [rows][n_heads][head_dim] (dtype of the shape).  Softmax statistics and
+ * sums are fp32; bf16 probabilities weight bf16 values.  A key that a query
+ * does not see has no influence on its output, whatever its values; an
+ * infinite or NaN value that it sees acts as the formula has it.  out must
+ * not overlap the inputs.  ws: at least the bytes above (may be NULL if
+ * those are 0), 256-byte aligned, scratch; concurrent calls need distinct ones.
+ * Allocates nothing. */
+upr_status upr_paged_attention(const upr_attn_shape* shape, const upr_paged_cache* cache,
+                               const upr_segments* queries, const int32_t* rows_host,
+                               const upr_attn_options* options, const void* q, int64_t q_ld, void* out,
+                               int64_t out_ld, void* ws, size_t ws_bytes, void* stream);
+
+/* ---- Model calls over histories in pages (pool of n_layers planes for the
+ * model's config; MXFP8 models: the bf16 cache).  rope (NULL: none) gives
+ * queries and keys their positions; a pool must be read with the rope that it
+ * was written with. */
+
+/* Workspace bytes of the two calls below (0 on invalid input). */
+size_t upr_extend_workspace_bytes(const upr_model* model, const upr_paged_cache* cache,
+                                  const upr_segments* fresh, const int32_t* rows_host);
+size_t upr_rank_paged_workspace_bytes(const upr_model* model, const upr_paged_cache* cache,
+                                      const upr_segments* cand, const int32_t* rows_host);
+
+/* Encodes the users' new actions onto their cached histories: the transformer
+ * of upr_encode_user over the new rows alone, whose keys and values are
+ * appended, layer by layer, as rows rows_host[u] - count_u .. rows_host[u] - 1.
+ * emb: device, rows of the segments, [rows, d_model] of the model dtype.
+ * Extending a history in pieces gives the keys and values of encoding it
+ * whole, up to rounding (without rope; upr_encode_user has no positions). */
+upr_status upr_extend_user(const upr_model* model, const upr_paged_cache* cache, const void* emb,
+                           const upr_segments* fresh, const int32_t* rows_host, const upr_rope* rope,
+                           void* ws, size_t ws_bytes, void* stream);
+
+/* upr_rank_candidates over histories in pages: candidates of user u see its
+ * first rows_host[u] cached rows and themselves; with rope they all stand at
+ * position rows_host[u] (paper Sec. 3: candidates share their position). */
+upr_status upr_rank_candidates_paged(const upr_model* model, const upr_paged_cache* cache,
+                                     const int32_t* rows_host, const void* cand_emb, const upr_segments* cand,
+                                     const upr_rope* rope, float* scores, void* ws, size_t ws_bytes,
+                                     void* stream);
+
 /* Diagnostics: per-kernel timing with HIP events.  While enabled, encode and
  * rank record a pair of hipEvents on the call's stream around every kernel
  * they launch, labelled with the kernel's name (e.g. "rank.attn").

@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "upr_internal.h"
+#include "upr_paged_host.h"
 #include "upr_plan.h"
 #include "upr_profile.h"
 
@@ -387,6 +388,62 @@ static WorkList work_list(const upr_segments* rows, const upr_segments* hist, in
                     rows->offsets_host[rows->num_users], cap};
 }
 
+// The paged calls' history: pages instead of a packed cache.
+struct PagedCall {
+    const upr_paged_cache* cache;
+    const int32_t* rows_host;
+    RopeArgs rope;              // rot_dim 0: no positions
+    size_t plane_bytes;
+};
+
+// Attention of the q|k|v rows of one layer over its plane of pages -> o
+// (`kind`).  Queries carry log2(e)/sqrt(D) already.  own: candidates, each with
+// its own key and value; else the rows are the newest of the cache.
+static AttnArgs paged_attn_args(const upr_config& c, const void* qkv, int64_t row0, void* o, int kind, bool own) {
+    const int d = c.d_model;
+    // rows of the workspace start at the call's first row
+    auto rows = [&](const void* p, int64_t ld, size_t es) { return static_cast<const char*>(p) - (size_t)row0 * ld * es; };
+    const size_t es = elem_size(c), o_es = kind == ATTN_OUT_F16 ? 2 : kind == ATTN_OUT_F32 ? 4 : es;
+    const char* const q = rows(qkv, 3 * d, es);
+    AttnArgs a{};
+    a.n_heads = a.n_kv_heads = c.n_heads;
+    a.D = c.head_dim;
+    a.q = RowsOf{q, 3 * d};
+    if (own) {
+        a.k_self = RowsOf{q + d * es, 3 * d};
+        a.v_self = RowsOf{q + 2 * d * es, 3 * d};
+    }
+    a.out = const_cast<char*>(rows(o, d, o_es));
+    a.out_ld = d;
+    a.out_kind = kind;
+    a.c = 1.0f;
+    return a;
+}
+
+static int paged_dtype(const upr_config& c) { return bf16_family(c.dtype) ? UPR_BF16 : UPR_F32; }
+
+// Ranking's attention of one layer over the pages: the candidates' queries
+// and own keys, rotated at their user's next position, then the attention.
+static hipError_t rank_attn_paged(const upr_config& c, const PagedCall& pc, const upr_segments* cand, int layer,
+                                  void* qkv, int64_t row0, void* o, int kind, void* ws, hipStream_t s) {
+    const PagedPool pool = paged_pool(*pc.cache, pc.plane_bytes, layer);
+    const AttnArgs a = paged_attn_args(c, qkv, row0, o, kind, true);
+    if (pc.rope.rot_dim > 0) {
+        AppendArgs t{};
+        t.n_heads = 2 * c.n_heads;          // q and k side by side
+        t.D = c.head_dim;
+        t.fixed = 1;
+        t.q = a.q;
+        t.q_out = const_cast<void*>(a.q.p);
+        t.q_out_ld = a.q.ld;
+        ProfScope ps("rank.rope", s);
+        const hipError_t e = paged_append(paged_dtype(c), pc.rope, t, pool, cand, pc.rows_host, s);
+        if (e != hipSuccess) return e;
+    }
+    ProfScope ps("rank.attn", s);
+    return paged_attn(paged_dtype(c), a, pool, cand, pc.rows_host, ws, s);
+}
+
 // Candidate layers of the fp8-projection variant: the bf16 sequence with
 // MXFP8 projection operands (LayerNorms write MXFP8 directly, the attention
 // kernel encodes its fp32 output, the FFN-up GEMM writes its GELU output as
@@ -395,7 +452,7 @@ static WorkList work_list(const upr_segments* rows, const upr_segments* hist, in
 static upr_status rank_layers_mx(const upr_model* m, const upr_kv_cache* cache,
                                  const upr_segments* hist, const bf16* cand_emb,
                                  const upr_segments* cand, float* scores, bool* scored,
-                                 const RankPlan& p, char* ws, hipStream_t s) {
+                                 const RankPlan& p, char* ws, const PagedCall* paged, hipStream_t s) {
     const upr_config& c = m->cfg;
     const int d = c.d_model, F = c.d_ff, H = c.n_heads, D = c.head_dim;
     const int64_t R = p.rows;
@@ -454,9 +511,12 @@ static upr_status rank_layers_mx(const upr_model* m, const upr_kv_cache* cache,
         e.col_scale = qscale;
         e.scale_cols = d;
         UPR_LAUNCH("rank.gemm_qkv", launch_gemm_mx(ac, asc, w.mx_qkv, w.mx_qkv_s, R, 3 * d, d, e, s));
-        const bf16* ck = static_cast<const bf16*>(plane_ptr(c, cache, l, 0));
-        const bf16* cv = static_cast<const bf16*>(plane_ptr(c, cache, l, 1));
-        if (p.use_mfma_attn) {
+        const bf16* ck = paged ? nullptr : static_cast<const bf16*>(plane_ptr(c, cache, l, 0));
+        const bf16* cv = paged ? nullptr : static_cast<const bf16*>(plane_ptr(c, cache, l, 1));
+        if (paged) {
+            UPR_HIP(rank_attn_paged(c, *paged, cand, l, qkv, p.row0, o32, ATTN_OUT_F32, ws + p.off_paged, s));
+            UPR_LAUNCH("rank.quant_o", launch_mx_quantize<float>(o32, R, d, ac, asc, s));
+        } else if (p.use_mfma_attn) {
             // attention writes the O projection's MXFP8 operand directly
             UPR_LAUNCH("rank.attn", launch_attn_rank_mx(qkv, ac, asc, p.row0, H, D,
                                                         reinterpret_cast<const int32_t*>(ws + p.off_work),
@@ -654,6 +714,8 @@ static hipError_t launch_ffn_block(const char* const names[7], const upr_config&
 
 static const char* const kEncodeFfnNames[7] = {"encode.gemm_o", "encode.ln2", "encode.gemm_up",
                                                "encode.gemm_down", "encode.oproj_ffn", "encode.ln1", ""};
+static const char* const kExtendFfnNames[7] = {"extend.gemm_o", "extend.ln2", "extend.gemm_up",
+                                               "extend.gemm_down", "extend.oproj_ffn", "extend.ln1", ""};
 static const char* const kRankFfnNames[7] = {"rank.gemm_o", "rank.ln2", "rank.gemm_up", "rank.gemm_down",
                                              "rank.oproj_ffn", "rank.ln1", "rank.score_head"};
 
@@ -737,6 +799,62 @@ static upr_status run_encode(const upr_model* m, const typename Types::kv* hist_
     return UPR_OK;
 }
 
+// Encode of new rows onto histories in pages: the encode pass over the new
+// rows alone, each layer's keys and values appended before its attention.
+template <typename Types>
+static upr_status run_extend(const upr_model* m, const typename Types::kv* emb, const upr_segments* fresh,
+                             const PagedCall& pc, const RankPlan& p, char* ws, hipStream_t s) {
+    using T = typename Types::kv;
+    using TA = typename Types::act;
+    const upr_config& c = m->cfg;
+    const int d = c.d_model, D = c.head_dim;
+    const int64_t R = p.rows;
+    float* g = reinterpret_cast<float*>(ws + p.off_g);
+    TA* a = reinterpret_cast<TA*>(ws + p.off_a);
+    T* qkv = reinterpret_cast<T*>(ws + p.off_qkv);
+    TA* o = reinterpret_cast<TA*>(ws + p.off_o);
+    TA* h = reinterpret_cast<TA*>(ws + p.off_h);
+    const float qscale = 1.4426950408889634f / std::sqrt((float)D);
+    const bool bf = std::is_same_v<Types, Bf16Types>;
+    const int dt = paged_dtype(c);
+    UPR_LAUNCH("extend.init_ln1",
+               launch_init_layernorm<T, TA>(emb + p.row0 * d, bf ? nullptr : g, a, R, d, m->layers[0].ln1_g,
+                                            m->layers[0].ln1_b, c.ln_eps, nullptr, s));
+    const AttnArgs at = paged_attn_args(c, qkv, p.row0, o, bf ? ATTN_OUT_F16 : ATTN_OUT_STORAGE, false);
+    AppendArgs ap{};
+    ap.n_heads = ap.n_kv_heads = c.n_heads;
+    ap.D = D;
+    ap.k = RowsOf{static_cast<const T*>(at.q.p) + d, at.q.ld};
+    ap.v = RowsOf{static_cast<const T*>(at.q.p) + 2 * d, at.q.ld};
+    if (pc.rope.rot_dim > 0) {              // the queries turn in place
+        ap.q = at.q;
+        ap.q_out = const_cast<void*>(at.q.p);
+        ap.q_out_ld = at.q.ld;
+    }
+    for (int l = 0; l < c.n_layers; ++l) {
+        const LayerWeights& w = m->layers[l];
+        if (l > 0 && !fused_layernorm<Types>(c))
+            UPR_LAUNCH("extend.ln1", launch_layernorm<TA>(g, a, R, d, w.ln1_g, w.ln1_b, c.ln_eps, s));
+        Epilogue e{};
+        e.mode = EPI_STORE;
+        e.acc_scale = w.s_qkv;
+        e.bias = w.bqkv;
+        e.out = qkv;
+        e.ldo = 3 * d;
+        e.col_scale = qscale;
+        e.scale_cols = d;
+        UPR_LAUNCH("extend.gemm_qkv", launch_gemm<TA, T>(a, d, static_cast<const TA*>(w.Wqkv), R, 3 * d, d, e, s));
+        const PagedPool pool = paged_pool(*pc.cache, pc.plane_bytes, l);
+        UPR_LAUNCH("extend.append", paged_append(dt, pc.rope, ap, pool, fresh, pc.rows_host, s));
+        if (l == c.n_layers - 1) break;     // the pages are complete; nothing reads further
+        UPR_LAUNCH("extend.attn", paged_attn(dt, at, pool, fresh, pc.rows_host, ws + p.off_paged, s));
+        const LayerWeights& wn = m->layers[l + 1];
+        UPR_HIP(launch_ffn_block<Types>(kExtendFfnNames, c, w, o, a, h, g, R, wn.ln1_g, wn.ln1_b,
+                                        bf && l == 0 ? emb + p.row0 * d : nullptr, nullptr, nullptr, s));
+    }
+    return UPR_OK;
+}
+
 // Outputs of a rank pass: the single score, or the action heads'
 // probabilities / utilities.
 struct RankOut {
@@ -751,7 +869,7 @@ template <typename Types>
 static upr_status run_rank(const upr_model* m, const upr_kv_cache* cache,
                            const upr_segments* hist, const typename Types::kv* cand_emb,
                            const upr_segments* cand, const RankOut& out, const RankPlan& p,
-                           char* ws, hipStream_t s) {
+                           char* ws, hipStream_t s, const PagedCall* paged = nullptr) {
     using T = typename Types::kv;
     using TA = typename Types::act;
     const upr_config& c = m->cfg;
@@ -767,7 +885,7 @@ static upr_status run_rank(const upr_model* m, const upr_kv_cache* cache,
     if constexpr (std::is_same_v<Types, Bf16Types>) {
         if (c.dtype == UPR_BF16_MXFP8) {
             const upr_status st = rank_layers_mx(m, cache, hist, cand_emb, cand,
-                                                 out.heads ? nullptr : out.scores + p.row0, &mx_scored, p, ws, s);
+                                                 out.heads ? nullptr : out.scores + p.row0, &mx_scored, p, ws, paged, s);
             if (st != UPR_OK) return st;
             mx_done = true;
         }
@@ -776,7 +894,8 @@ static upr_status run_rank(const upr_model* m, const upr_kv_cache* cache,
     // bf16 models: the first O projection reads the residual from the tokens
     const bool tok_resid = std::is_same_v<Types, Bf16Types>;
     const bool list_with_ln = p.use_mfma_attn && cand->num_users <= kListMaxUsers;
-    const WorkList wl = work_list(cand, hist, H, p, false, ws, cache->capacity_rows);
+    const WorkList wl = list_with_ln || p.use_mfma_attn ? work_list(cand, hist, H, p, false, ws, cache->capacity_rows)
+                                                     : WorkList{};
     UPR_LAUNCH("rank.init_ln1",
                launch_init_layernorm<T, TA>(cand_emb + p.row0 * d, tok_resid ? nullptr : g, a, R, d,
                                             m->layers[0].ln1_g, m->layers[0].ln1_b, c.ln_eps,
@@ -796,9 +915,13 @@ static upr_status run_rank(const upr_model* m, const upr_kv_cache* cache,
         e.scale_cols = d;
         UPR_LAUNCH("rank.gemm_qkv",
                    launch_gemm<TA, T>(a, d, static_cast<const TA*>(w.Wqkv), R, 3 * d, d, e, s));
-        const T* ck = static_cast<const T*>(plane_ptr(c, cache, l, 0));
-        const T* cv = static_cast<const T*>(plane_ptr(c, cache, l, 1));
-        bool done = false;
+        const T* ck = paged ? nullptr : static_cast<const T*>(plane_ptr(c, cache, l, 0));
+        const T* cv = paged ? nullptr : static_cast<const T*>(plane_ptr(c, cache, l, 1));
+        bool done = paged != nullptr;
+        if (paged)
+            UPR_HIP(rank_attn_paged(c, *paged, cand, l, qkv, p.row0, o,
+                                    std::is_same_v<Types, Bf16Types> ? ATTN_OUT_F16 : ATTN_OUT_STORAGE,
+                                    ws + p.off_paged, s));
         if constexpr (std::is_same_v<Types, Bf16Types>) {
             if (p.use_mfma_attn) {
                 UPR_LAUNCH("rank.attn", launch_attn_rank(qkv, o, p.row0, H, D,
@@ -1153,6 +1276,103 @@ upr_status upr_rank_candidates_noalloc(const upr_model* m, const upr_kv_cache* c
                                        const upr_segments* hist, const void* cand_emb,
                                        const upr_segments* cand, float* scores, void* stream) {
     return rank_entry(m, cache, hist, cand_emb, cand, scores, nullptr, 0, true, stream);
+}
+
+// ---- histories in pages
+
+size_t upr_paged_cache_bytes(const upr_config* cfg, int64_t n_pages, int32_t page_rows) {
+    if (check_config(cfg) != UPR_OK || upr::check_page_rows(page_rows) != UPR_OK || n_pages < 0 ||
+        n_pages > 0x7fffffff)
+        return 0;
+    return (size_t)cfg->n_layers * n_pages * 2 * cfg->n_heads * page_rows * cfg->head_dim * elem_size(*cfg);
+}
+
+// Checks and plan shared by the paged model calls (pointers of the cache and
+// the tokens are looked at only if there are rows).
+static upr_status paged_plan(const upr_model* m, const upr_paged_cache* cache, const upr_segments* seg,
+                             const char* name, const int32_t* rows_host, const upr_rope* rope, bool own,
+                             upr::RankPlan* p) {
+    if (!m) return fail(UPR_ERR_NULL, "model is NULL");
+    upr_status st = upr::check_paged_cache(cache, false);
+    int64_t rows = 0;
+    if (st == UPR_OK)
+        st = upr::check_paged_users(seg, name, rows_host, cache->page_rows, cache->table_stride, !own, &rows);
+    if (st == UPR_OK) st = upr::check_model_rope(rope, m->cfg.head_dim);
+    if (st != UPR_OK) return st;
+    upr::AttnArgs a{};
+    a.n_heads = a.n_kv_heads = m->cfg.n_heads;
+    a.D = m->cfg.head_dim;
+    a.k_self.p = own ? m : nullptr;
+    *p = upr::plan_paged(m->cfg, seg->num_users, seg->offsets_host,
+                         rows == 0 ? 0 : upr::paged_attn_workspace(upr::paged_dtype(m->cfg), a, seg, rows_host));
+    return UPR_OK;
+}
+
+static upr::PagedCall paged_call(const upr_model* m, const upr_paged_cache* cache, const int32_t* rows_host,
+                                 const upr_rope* rope) {
+    return upr::PagedCall{cache, rows_host, upr::rope_args(rope),
+                          upr_paged_cache_bytes(&m->cfg, cache->n_pages, cache->page_rows) / m->cfg.n_layers};
+}
+
+size_t upr_extend_workspace_bytes(const upr_model* m, const upr_paged_cache* cache, const upr_segments* fresh,
+                                  const int32_t* rows_host) {
+    upr::RankPlan p;
+    return paged_plan(m, cache, fresh, "fresh", rows_host, nullptr, false, &p) == UPR_OK ? p.bytes : 0;
+}
+
+upr_status upr_extend_user(const upr_model* m, const upr_paged_cache* cache, const void* emb,
+                           const upr_segments* fresh, const int32_t* rows_host, const upr_rope* rope, void* ws,
+                           size_t ws_bytes, void* stream) {
+    upr::RankPlan p;
+    upr_status st = paged_plan(m, cache, fresh, "fresh", rows_host, rope, false, &p);
+    if (st != UPR_OK) return st;
+    if (p.rows == 0) return ok();
+    if (!emb) return fail(UPR_ERR_NULL, "emb is NULL");
+    st = upr::check_paged_cache(cache, true);
+    if (st == UPR_OK) st = check_workspace(ws, ws_bytes, p.bytes);
+    if (st != UPR_OK) return st;
+    clear_pending_error();
+    arm_stop_hook();
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    char* w = static_cast<char*>(ws);
+    const upr::PagedCall pc = paged_call(m, cache, rows_host, rope);
+    st = bf16_family(m->cfg.dtype)
+             ? upr::run_extend<upr::Bf16Types>(m, static_cast<const bf16*>(emb), fresh, pc, p, w, s)
+             : upr::run_extend<upr::F32Types>(m, static_cast<const float*>(emb), fresh, pc, p, w, s);
+    return st == UPR_OK ? ok() : st;
+}
+
+size_t upr_rank_paged_workspace_bytes(const upr_model* m, const upr_paged_cache* cache, const upr_segments* cand,
+                                      const int32_t* rows_host) {
+    upr::RankPlan p;
+    return paged_plan(m, cache, cand, "cand", rows_host, nullptr, true, &p) == UPR_OK ? p.bytes : 0;
+}
+
+upr_status upr_rank_candidates_paged(const upr_model* m, const upr_paged_cache* cache, const int32_t* rows_host,
+                                     const void* cand_emb, const upr_segments* cand, const upr_rope* rope,
+                                     float* scores, void* ws, size_t ws_bytes, void* stream) {
+    upr::RankPlan p;
+    upr_status st = paged_plan(m, cache, cand, "cand", rows_host, rope, true, &p);
+    if (st != UPR_OK) return st;
+    if (p.rows == 0) return ok();
+    if (!cand_emb) return fail(UPR_ERR_NULL, "cand_emb is NULL");
+    if (!scores) return fail(UPR_ERR_NULL, "scores is NULL");
+    st = upr::check_paged_cache(cache, true);
+    if (st == UPR_OK) st = check_workspace(ws, ws_bytes, p.bytes);
+    if (st != UPR_OK) return st;
+    clear_pending_error();
+    arm_stop_hook();
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    char* w = static_cast<char*>(ws);
+    const upr::PagedCall pc = paged_call(m, cache, rows_host, rope);
+    upr::RankOut out;
+    out.scores = scores;
+    st = bf16_family(m->cfg.dtype)
+             ? upr::run_rank<upr::Bf16Types>(m, nullptr, nullptr, static_cast<const bf16*>(cand_emb), cand, out, p,
+                                             w, s, &pc)
+             : upr::run_rank<upr::F32Types>(m, nullptr, nullptr, static_cast<const float*>(cand_emb), cand, out, p,
+                                            w, s, &pc);
+    return st == UPR_OK ? ok() : st;
 }
 
 // ---- per-action heads and utility top-K

@@ -1,0 +1,378 @@
+// Host side of the paged-cache operators: argument checks, frequency tables,
+// and the launches of upr_rope_*, upr_paged_append and upr_paged_attention.
+#include <cmath>
+
+#include "upr_paged_host.h"
+#include "upr_profile.h"
+
+namespace upr {
+
+namespace {
+
+constexpr int32_t kMaxRows = 1 << 30;
+
+bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+int elem(int dtype) { return dtype == UPR_F32 ? 4 : 2; }
+
+upr_status check_dtype(int32_t dtype) {
+    if (dtype != UPR_F32 && dtype != UPR_BF16)
+        return report_error(UPR_ERR_DTYPE, "dtype %d is not UPR_F32 or UPR_BF16", dtype);
+    return UPR_OK;
+}
+
+upr_status check_head_dim(int32_t D) {
+    if (D != 32 && D != 64 && D != 128)
+        return report_error(UPR_ERR_CONFIG, "head_dim %d not supported (32, 64 or 128)", D);
+    return UPR_OK;
+}
+
+upr_status check_shape(const upr_attn_shape* sh) {
+    if (!sh) return report_error(UPR_ERR_NULL, "shape is NULL");
+    upr_status st = check_dtype(sh->dtype);
+    if (st == UPR_OK) st = check_head_dim(sh->head_dim);
+    if (st != UPR_OK) return st;
+    if (sh->n_kv_heads < 1 || sh->n_heads < sh->n_kv_heads || sh->n_heads > 1024 ||
+        sh->n_heads % sh->n_kv_heads != 0)
+        return report_error(UPR_ERR_CONFIG, "%d heads over %d key/value heads: need 1 <= n_kv_heads <= n_heads <= "
+                            "1024, n_heads a multiple of n_kv_heads", sh->n_heads, sh->n_kv_heads);
+    return UPR_OK;
+}
+
+// One tensor of rows of `heads` heads (name for the message).
+upr_status check_rows(const char* name, const void* p, int64_t ld, int heads, int D, int dtype) {
+    if (!p) return report_error(UPR_ERR_NULL, "%s is NULL", name);
+    if (!aligned16(p)) return report_error(UPR_ERR_LIMIT, "%s is not 16-byte aligned", name);
+    if (ld < (int64_t)heads * D || ld > (int64_t{1} << 40) || ld * elem(dtype) % 16 != 0)
+        return report_error(UPR_ERR_LIMIT, "leading dimension %lld of %s: need at least %d elements, a multiple of "
+                            "16 bytes", (long long)ld, name, heads * D);
+    return UPR_OK;
+}
+
+upr_status check_rope(const upr_rope* r, int head_dim) {
+    if (r->rot_dim < 2 || r->rot_dim % 2 != 0 || r->rot_dim > 2 * UPR_ROPE_MAX_PAIRS || r->rot_dim > head_dim)
+        return report_error(UPR_ERR_LIMIT, "rot_dim %d must be even, in [2, %d]", r->rot_dim, head_dim);
+    if (r->layout != UPR_ROPE_HALF && r->layout != UPR_ROPE_INTERLEAVED)
+        return report_error(UPR_ERR_LIMIT, "rope layout %d is not a upr_rope_layout value", r->layout);
+    if (!std::isfinite(r->magnitude) || !std::isfinite((float)r->magnitude))
+        return report_error(UPR_ERR_LIMIT, "rope magnitude is not a finite float");
+    for (int i = 0; i < r->rot_dim / 2; ++i)
+        if (!std::isfinite(r->freq[i]) || std::fabs(r->freq[i]) > 1e6)
+            return report_error(UPR_ERR_LIMIT, "rope frequency %d is not finite or beyond 1e6", i);
+    return UPR_OK;
+}
+
+}  // namespace
+
+upr_status check_page_rows(int32_t page_rows) {
+    if (page_rows < 16 || page_rows > 1024 || (page_rows & (page_rows - 1)) != 0)
+        return report_error(UPR_ERR_LIMIT, "page_rows %d must be a power of two in [16, 1024]", page_rows);
+    return UPR_OK;
+}
+
+upr_status check_paged_users(const upr_segments* seg, const char* name, const int32_t* rows_host, int32_t page_rows,
+                             int32_t table_stride, bool part_of_cache, int64_t* total) {
+    if (!seg) return report_error(UPR_ERR_NULL, "%s segments pointer is NULL", name);
+    if (seg->num_users < 0) return report_error(UPR_ERR_OFFSETS, "%s num_users %d < 0", name, seg->num_users);
+    if (!seg->offsets_host) return report_error(UPR_ERR_NULL, "%s offsets_host is NULL", name);
+    const int32_t* o = seg->offsets_host;
+    if (o[0] < 0) return report_error(UPR_ERR_OFFSETS, "%s offsets[0] = %d < 0", name, o[0]);
+    if (seg->num_users > 0 && !rows_host) return report_error(UPR_ERR_NULL, "rows_host is NULL");
+    for (int u = 0; u < seg->num_users; ++u) {
+        if (o[u + 1] < o[u])
+            return report_error(UPR_ERR_OFFSETS, "%s offsets decrease at user %d (%d -> %d)", name, u, o[u], o[u + 1]);
+        const int32_t n = rows_host[u], c = o[u + 1] - o[u];
+        if (n < 0 || (part_of_cache && n < c))
+            return report_error(UPR_ERR_OFFSETS, "user %d has %d cached rows, %d of them new", u, n, c);
+        if (n > kMaxRows) return report_error(UPR_ERR_LIMIT, "user %d has %d cached rows (at most %d)", u, n, kMaxRows);
+        if (c > 0 && ((int64_t)n + page_rows - 1) / page_rows > table_stride)
+            return report_error(UPR_ERR_CAPACITY, "user %d has %d cached rows, its table %d pages of %d", u, n,
+                                table_stride, page_rows);
+    }
+    *total = (int64_t)o[seg->num_users] - o[0];
+    return UPR_OK;
+}
+
+upr_status check_paged_cache(const upr_paged_cache* c, bool pointers) {
+    if (!c) return report_error(UPR_ERR_NULL, "cache is NULL");
+    const upr_status st = check_page_rows(c->page_rows);
+    if (st != UPR_OK) return st;
+    if (c->n_pages < 0 || c->n_pages > 0x7fffffff)
+        return report_error(UPR_ERR_LIMIT, "n_pages %lld outside [0, 2^31)", (long long)c->n_pages);
+    if (c->table_stride < 0) return report_error(UPR_ERR_LIMIT, "table_stride %d < 0", c->table_stride);
+    if (!pointers) return UPR_OK;
+    if (c->n_pages > 0 && !c->data) return report_error(UPR_ERR_NULL, "cache data is NULL");
+    if (!aligned16(c->data)) return report_error(UPR_ERR_LIMIT, "cache data is not 16-byte aligned");
+    if (c->table_stride > 0 && !c->tables) return report_error(UPR_ERR_NULL, "cache tables is NULL");
+    return UPR_OK;
+}
+
+upr_status check_attn_options(const upr_attn_options* o) {
+    if (!o) return report_error(UPR_ERR_NULL, "options is NULL");
+    // (in log2 units, and as the argument of the tanh, they have to be fp32 too)
+    if (!(o->scale > 0.f) || !(o->scale < 1e30f))
+        return report_error(UPR_ERR_LIMIT, "scale must be positive and below 1e30");
+    if (!(o->softcap >= 0.f) || !(o->softcap < 1e30f) || (o->softcap > 0.f && !std::isfinite(o->scale / o->softcap)))
+        return report_error(UPR_ERR_LIMIT, "softcap must be 0, or positive, below 1e30 and with a finite scale / softcap");
+    if (o->window < 0) return report_error(UPR_ERR_LIMIT, "window %d < 0", o->window);
+    if ((o->k_self == nullptr) != (o->v_self == nullptr))
+        return report_error(UPR_ERR_NULL, "k_self and v_self must both be given or both be NULL");
+    return UPR_OK;
+}
+
+PagedPool paged_pool(const upr_paged_cache& c, size_t plane_bytes, int plane) {
+    int shift = 0;
+    while ((1 << shift) < c.page_rows) ++shift;
+    return PagedPool{static_cast<char*>(c.data) + plane_bytes * plane, c.tables, c.n_pages, c.table_stride,
+                     c.page_rows, shift};
+}
+
+RopeArgs rope_args(const upr_rope* r) {
+    RopeArgs a{};
+    if (!r) return a;
+    a.rot_dim = r->rot_dim;
+    a.layout = r->layout;
+    a.magnitude = (float)r->magnitude;
+    for (int i = 0; i < r->rot_dim / 2; ++i) a.quarters[i] = r->freq[i] * (2.0 / M_PI);
+    return a;
+}
+
+upr_status check_model_rope(const upr_rope* r, int head_dim) { return r ? check_rope(r, head_dim) : UPR_OK; }
+
+// Cuts a call's users into launches of at most kPagedUsers and kMaxItems work
+// items; `items` gives a user's items.
+template <typename Items, typename Launch>
+static hipError_t each_launch(const upr_segments* seg, const int32_t* rows_host, const Items& items,
+                              const Launch& launch) {
+    constexpr int64_t kMaxItems = 1 << 30;
+    PagedUsers u;
+    u.n = 0;
+    u.item0[0] = 0;
+    hipError_t e = hipSuccess;
+    const int32_t* const o = seg->offsets_host;
+    for (int i = 0; i < seg->num_users && e == hipSuccess; ++i) {
+        const int32_t c = o[i + 1] - o[i];
+        if (c == 0) continue;
+        const int64_t n = items(c, rows_host[i]);
+        if (n > kMaxItems) return hipErrorInvalidConfiguration;
+        if (u.n == kPagedUsers || (u.n > 0 && u.item0[u.n] + n > kMaxItems)) {
+            e = launch(u);
+            u.n = 0;
+        }
+        u.user[u.n] = i;
+        u.row0[u.n] = o[i];
+        u.count[u.n] = c;
+        u.rows[u.n] = rows_host[i];
+        u.item0[u.n + 1] = u.item0[u.n] + (int32_t)n;
+        ++u.n;
+    }
+    if (u.n > 0 && e == hipSuccess) e = launch(u);
+    return e;
+}
+
+hipError_t paged_append(int dtype, const RopeArgs& rope, const AppendArgs& a, const PagedPool& pool,
+                        const upr_segments* seg, const int32_t* rows_host, hipStream_t s) {
+    return each_launch(
+        seg, rows_host, [&](int32_t c, int32_t) { return append_items(dtype, rope, a, c); },
+        [&](const PagedUsers& u) { return launch_append(dtype, rope, a, pool, u, s); });
+}
+
+size_t paged_attn_workspace(int, const AttnArgs&, const upr_segments*, const int32_t*) { return 0; }
+
+hipError_t paged_attn(int dtype, const AttnArgs& a, const PagedPool& pool, const upr_segments* seg,
+                      const int32_t* rows_host, void*, hipStream_t s) {
+    return each_launch(
+        seg, rows_host, [&](int32_t c, int32_t) { return ((int64_t)c * a.n_heads + 3) / 4; },
+        [&](const PagedUsers& u) { return launch_paged_attn(dtype, a, pool, u, s); });
+}
+
+}  // namespace upr
+
+using namespace upr;
+
+// What the attention's plan depends on (no pointers but whether rows have
+// their own keys).
+static AttnArgs attn_args(const upr_attn_shape& sh, const upr_attn_options& o) {
+    AttnArgs a{};
+    a.n_heads = sh.n_heads;
+    a.n_kv_heads = sh.n_kv_heads;
+    a.D = sh.head_dim;
+    a.k_self = RowsOf{o.k_self, o.self_ld};
+    a.v_self = RowsOf{o.v_self, o.self_ld};
+    a.c = (float)(o.scale * 1.4426950408889634);
+    if (o.softcap > 0.f) {
+        a.ct = (float)((double)o.scale / o.softcap);
+        a.cap2 = (float)(o.softcap * 1.4426950408889634);
+    }
+    a.slopes = o.slopes;
+    a.window = o.window;
+    return a;
+}
+
+extern "C" {
+
+upr_status upr_rope_init(int32_t rot_dim, int32_t layout, double base, int32_t scaling, double factor,
+                         double original_length, upr_rope* out) {
+    if (!out) return report_error(UPR_ERR_NULL, "out is NULL");
+    if (rot_dim < 2 || rot_dim % 2 != 0 || rot_dim > 2 * UPR_ROPE_MAX_PAIRS)
+        return report_error(UPR_ERR_LIMIT, "rot_dim %d must be even, in [2, %d]", rot_dim, 2 * UPR_ROPE_MAX_PAIRS);
+    if (layout != UPR_ROPE_HALF && layout != UPR_ROPE_INTERLEAVED)
+        return report_error(UPR_ERR_LIMIT, "rope layout %d is not a upr_rope_layout value", layout);
+    if (!(base > 1.0) || !std::isfinite(base)) return report_error(UPR_ERR_LIMIT, "base must be finite and above 1");
+    if (scaling < UPR_ROPE_PLAIN || scaling > UPR_ROPE_BY_PARTS)
+        return report_error(UPR_ERR_LIMIT, "rope scaling %d is not a upr_rope_scaling value", scaling);
+    if (scaling != UPR_ROPE_PLAIN && (!(factor >= 1.0) || !std::isfinite(factor)))
+        return report_error(UPR_ERR_LIMIT, "factor must be finite and at least 1");
+    if (scaling == UPR_ROPE_NTK && rot_dim < 4)
+        return report_error(UPR_ERR_LIMIT, "the base change needs rot_dim >= 4");
+    if (scaling == UPR_ROPE_BY_PARTS && (!(original_length > 0.0) || !std::isfinite(original_length)))
+        return report_error(UPR_ERR_LIMIT, "original_length must be positive and finite");
+    upr_rope r{};
+    r.rot_dim = rot_dim;
+    r.layout = layout;
+    r.magnitude = scaling == UPR_ROPE_BY_PARTS ? 1.0 + 0.1 * std::log(factor) : 1.0;
+    if (scaling == UPR_ROPE_NTK) base *= std::pow(factor, rot_dim / (rot_dim - 2.0));
+    if (!std::isfinite(base)) return report_error(UPR_ERR_LIMIT, "base and factor overflow");
+    for (int i = 0; i < rot_dim / 2; ++i) {
+        double f = std::pow(base, -2.0 * i / rot_dim);
+        if (scaling == UPR_ROPE_LINEAR) f /= factor;
+        if (scaling == UPR_ROPE_BY_PARTS) {
+            const double turns = f * original_length / (2.0 * M_PI);
+            const double keep = std::fmin(1.0, std::fmax(0.0, (turns - 1.0) / 31.0));
+            f = f * keep + f / factor * (1.0 - keep);
+        }
+        r.freq[i] = f;
+    }
+    *out = r;
+    return report_ok();
+}
+
+upr_status upr_rope_apply(const upr_rope* rope, int32_t dtype, int32_t heads, int32_t head_dim, const void* x,
+                          int64_t x_ld, const int32_t* positions, int64_t rows, void* out, int64_t out_ld,
+                          void* stream) {
+    if (!rope) return report_error(UPR_ERR_NULL, "rope is NULL");
+    upr_status st = check_dtype(dtype);
+    if (st == UPR_OK) st = check_head_dim(head_dim);
+    if (st == UPR_OK) st = check_rope(rope, head_dim);
+    if (st != UPR_OK) return st;
+    if (heads < 1 || heads > 2048) return report_error(UPR_ERR_LIMIT, "heads %d outside [1, 2048]", heads);
+    if (rows < 0 || rows > 0x7fffffff)
+        return report_error(UPR_ERR_LIMIT, "rows %lld outside [0, 2^31)", (long long)rows);
+    if (rows == 0) return report_ok();
+    st = check_rows("x", x, x_ld, heads, head_dim, dtype);
+    if (st == UPR_OK) st = check_rows("out", out, out_ld, heads, head_dim, dtype);
+    if (st != UPR_OK) return st;
+    if (!positions) return report_error(UPR_ERR_NULL, "positions is NULL");
+    if (x == out && x_ld != out_ld) return report_error(UPR_ERR_LIMIT, "in place, x_ld and out_ld must agree");
+    (void)hipGetLastError();
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    hipError_t e;
+    {
+        ProfScope ps("rope", s);
+        e = launch_rope(dtype, rope_args(rope), heads, head_dim, RowsOf{x, x_ld}, positions, rows, out, out_ld, s);
+    }
+    if (e != hipSuccess) return report_error(UPR_ERR_HIP, "rope launch failed: %s", hipGetErrorString(e));
+    return report_ok();
+}
+
+upr_status upr_paged_append(const upr_attn_shape* shape, const upr_paged_cache* cache, const upr_segments* fresh,
+                            const int32_t* rows_host, const upr_rope* rope, const void* k, int64_t k_ld,
+                            const void* v, int64_t v_ld, const void* q, int64_t q_ld, void* q_out,
+                            int64_t q_out_ld, void* stream) {
+    upr_status st = check_shape(shape);
+    if (st == UPR_OK) st = check_paged_cache(cache, false);
+    int64_t rows = 0;
+    if (st == UPR_OK)
+        st = check_paged_users(fresh, "fresh", rows_host, cache->page_rows, cache->table_stride, true, &rows);
+    if (st == UPR_OK && rope) st = check_rope(rope, shape->head_dim);
+    if (st != UPR_OK) return st;
+    if ((q == nullptr) != (q_out == nullptr))
+        return report_error(UPR_ERR_NULL, "q and q_out must both be given or both be NULL");
+    if (rows == 0) return report_ok();
+    const int D = shape->head_dim, dt = shape->dtype;
+    st = check_paged_cache(cache, true);
+    if (st == UPR_OK) st = check_rows("k", k, k_ld, shape->n_kv_heads, D, dt);
+    if (st == UPR_OK) st = check_rows("v", v, v_ld, shape->n_kv_heads, D, dt);
+    if (st == UPR_OK && q) st = check_rows("q", q, q_ld, shape->n_heads, D, dt);
+    if (st == UPR_OK && q) st = check_rows("q_out", q_out, q_out_ld, shape->n_heads, D, dt);
+    if (st != UPR_OK) return st;
+    if (q && q == q_out && q_ld != q_out_ld)
+        return report_error(UPR_ERR_LIMIT, "in place, q_ld and q_out_ld must agree");
+    AppendArgs a{};
+    a.n_heads = shape->n_heads;
+    a.n_kv_heads = shape->n_kv_heads;
+    a.D = D;
+    a.k = RowsOf{k, k_ld};
+    a.v = RowsOf{v, v_ld};
+    a.q = RowsOf{q, q_ld};
+    a.q_out = q_out;
+    a.q_out_ld = q_out_ld;
+    (void)hipGetLastError();
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    hipError_t e;
+    {
+        ProfScope ps("paged.append", s);
+        e = paged_append(dt, rope_args(rope), a, paged_pool(*cache, 0, 0), fresh, rows_host, s);
+    }
+    if (e != hipSuccess) return report_error(UPR_ERR_HIP, "append launch failed: %s", hipGetErrorString(e));
+    return report_ok();
+}
+
+size_t upr_paged_attention_workspace_bytes(const upr_attn_shape* shape, const upr_paged_cache* cache,
+                                           const upr_segments* queries, const int32_t* rows_host,
+                                           const upr_attn_options* options) {
+    int64_t rows;
+    if (check_shape(shape) != UPR_OK || check_paged_cache(cache, false) != UPR_OK ||
+        check_attn_options(options) != UPR_OK ||
+        check_paged_users(queries, "query", rows_host, cache->page_rows, cache->table_stride, !options->k_self,
+                          &rows) != UPR_OK)
+        return 0;
+    return paged_attn_workspace(shape->dtype, attn_args(*shape, *options), queries, rows_host);
+}
+
+upr_status upr_paged_attention(const upr_attn_shape* shape, const upr_paged_cache* cache,
+                               const upr_segments* queries, const int32_t* rows_host,
+                               const upr_attn_options* options, const void* q, int64_t q_ld, void* out,
+                               int64_t out_ld, void* ws, size_t ws_bytes, void* stream) {
+    upr_status st = check_shape(shape);
+    if (st == UPR_OK) st = check_paged_cache(cache, false);
+    if (st == UPR_OK) st = check_attn_options(options);
+    int64_t rows = 0;
+    if (st == UPR_OK)
+        st = check_paged_users(queries, "query", rows_host, cache->page_rows, cache->table_stride, !options->k_self,
+                               &rows);
+    if (st != UPR_OK) return st;
+    if (rows == 0) return report_ok();
+    const int D = shape->head_dim, dt = shape->dtype;
+    st = check_paged_cache(cache, true);
+    if (st == UPR_OK) st = check_rows("q", q, q_ld, shape->n_heads, D, dt);
+    if (st == UPR_OK) st = check_rows("out", out, out_ld, shape->n_heads, D, dt);
+    if (st == UPR_OK && options->k_self) {
+        st = check_rows("k_self", options->k_self, options->self_ld, shape->n_kv_heads, D, dt);
+        if (st == UPR_OK) st = check_rows("v_self", options->v_self, options->self_ld, shape->n_kv_heads, D, dt);
+    }
+    if (st != UPR_OK) return st;
+    AttnArgs a = attn_args(*shape, *options);
+    const size_t need = paged_attn_workspace(dt, a, queries, rows_host);
+    if (need > 0) {
+        if (!ws) return report_error(UPR_ERR_NULL, "workspace is NULL (%zu bytes needed)", need);
+        if (ws_bytes < need)
+            return report_error(UPR_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", ws_bytes, need);
+        if (reinterpret_cast<uintptr_t>(ws) % 256 != 0)
+            return report_error(UPR_ERR_WORKSPACE, "workspace is not 256-byte aligned");
+    }
+    a.q = RowsOf{q, q_ld};
+    a.out = out;
+    a.out_ld = out_ld;
+    (void)hipGetLastError();
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    hipError_t e;
+    {
+        ProfScope ps("paged.attention", s);
+        e = paged_attn(dt, a, paged_pool(*cache, 0, 0), queries, rows_host, ws, s);
+    }
+    if (e != hipSuccess) return report_error(UPR_ERR_HIP, "attention launch failed: %s", hipGetErrorString(e));
+    return report_ok();
+}
+
+}  // extern "C"

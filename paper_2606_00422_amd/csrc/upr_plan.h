@@ -44,6 +44,7 @@ struct RankPlan {
     int64_t work_items = 0;
     int attn_tile = kRankAttnTile;
     bool use_mfma_attn = false;
+    size_t off_paged = 0;           // paged calls: their attention's workspace
     size_t bytes = 0;
 };
 
@@ -150,6 +151,19 @@ inline RankPlan plan_rank(const upr_config& c, int U, const int32_t* coffs, cons
     p.off_h = o; o = align256(o + R * std::max<size_t>(F, (size_t)head_cols) * es);
     p.off_work = o; o = align256(o + (size_t)p.work_items * 4 * sizeof(int32_t));
     p.bytes = o;
+    return p;
+}
+
+// Workspace of the paged calls, extend or rank, for the rows of `offs`: as
+// rank's, with the paged attention's workspace in the work list's place.
+inline RankPlan plan_paged(const upr_config& c, int U, const int32_t* offs, size_t attn_bytes) {
+    const int32_t one[2] = {offs[0], offs[U]}, none[2] = {0, 0};
+    RankPlan p = plan_rank(c, 1, one, none, 0, false);
+    if (p.rows == 0) return p;
+    p.use_mfma_attn = false;
+    p.work_items = 0;
+    p.off_paged = p.off_work;
+    p.bytes = align256(p.off_work + attn_bytes);
     return p;
 }
 

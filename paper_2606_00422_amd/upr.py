@@ -21,6 +21,9 @@ UPR_ERR_WORKSPACE, UPR_ERR_DTYPE, UPR_ERR_HIP, UPR_ERR_WEIGHTS, UPR_ERR_LIMIT = 
 UPR_TOPK_MAX_CANDIDATES = 16384
 UPR_F32, UPR_BF16, UPR_BF16_MXFP8 = 0, 1, 2
 UPR_MX_IN_F32, UPR_MX_IN_F16, UPR_MX_IN_BF16 = 0, 1, 2
+UPR_ROPE_HALF, UPR_ROPE_INTERLEAVED = 0, 1
+UPR_ROPE_PLAIN, UPR_ROPE_LINEAR, UPR_ROPE_NTK, UPR_ROPE_BY_PARTS = 0, 1, 2, 3
+UPR_ROPE_MAX_PAIRS = 64
 
 # Every symbol include/upr.h declares.
 EXPORTS = (
@@ -35,6 +38,10 @@ EXPORTS = (
     "upr_kv_pool_create", "upr_kv_pool_export", "upr_kv_pool_export_file", "upr_kv_pool_open",
     "upr_kv_pool_open_file", "upr_kv_pool_slot", "upr_kv_pool_next_slot", "upr_kv_pool_info",
     "upr_kv_pool_destroy",
+    "upr_paged_cache_bytes", "upr_rope_init", "upr_rope_apply", "upr_paged_append",
+    "upr_paged_attention_workspace_bytes", "upr_paged_attention",
+    "upr_extend_workspace_bytes", "upr_extend_user",
+    "upr_rank_paged_workspace_bytes", "upr_rank_candidates_paged",
 )
 
 
@@ -67,6 +74,27 @@ class upr_kv_pool_handle(ctypes.Structure):
                 ("cfg", upr_config), ("ipc", ctypes.c_uint8 * 64)]
 
 
+class upr_paged_cache(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("page_rows", ctypes.c_int32),
+                ("table_stride", ctypes.c_int32), ("tables", ctypes.c_void_p)]
+
+
+class upr_attn_shape(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32)]
+
+
+class upr_rope(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("magnitude", ctypes.c_double),
+                ("freq", ctypes.c_double * UPR_ROPE_MAX_PAIRS)]
+
+
+class upr_attn_options(ctypes.Structure):
+    _fields_ = [("scale", ctypes.c_float), ("softcap", ctypes.c_float), ("window", ctypes.c_int32),
+                ("slopes", ctypes.c_void_p), ("k_self", ctypes.c_void_p), ("v_self", ctypes.c_void_p),
+                ("self_ld", ctypes.c_int64)]
+
+
 class upr_kernel_stat(ctypes.Structure):
     _fields_ = [("name", ctypes.c_char * 48), ("launches", ctypes.c_int64),
                 ("total_ms", ctypes.c_double)]
@@ -92,6 +120,7 @@ def load(path: str = LIB_PATH):
     lib = ctypes.CDLL(path)
     P, I32, I64, SZ, VP = ctypes.POINTER, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_void_p
     cfgp, segp, cachep = P(upr_config), P(upr_segments), P(upr_kv_cache)
+    D64, ropep, pagedp = ctypes.c_double, P(upr_rope), P(upr_paged_cache)
     sig = {
         "upr_weights_count": (I64, [cfgp]),
         "upr_model_create": (I32, [cfgp, VP, I64, P(VP)]),
@@ -125,6 +154,18 @@ def load(path: str = LIB_PATH):
         "upr_kv_pool_next_slot": (I32, [VP]),
         "upr_kv_pool_info": (I32, [VP, cfgp, P(I32), P(I64)]),
         "upr_kv_pool_destroy": (None, [VP]),
+        "upr_paged_cache_bytes": (SZ, [cfgp, I64, I32]),
+        "upr_rope_init": (I32, [I32, I32, D64, I32, D64, D64, ropep]),
+        "upr_rope_apply": (I32, [ropep, I32, I32, I32, VP, I64, VP, I64, VP, I64, VP]),
+        "upr_paged_append": (I32, [P(upr_attn_shape), pagedp, segp, VP, ropep, VP, I64, VP, I64, VP, I64, VP, I64,
+                                   VP]),
+        "upr_paged_attention_workspace_bytes": (SZ, [P(upr_attn_shape), pagedp, segp, VP, P(upr_attn_options)]),
+        "upr_paged_attention": (I32, [P(upr_attn_shape), pagedp, segp, VP, P(upr_attn_options), VP, I64, VP, I64, VP,
+                                      SZ, VP]),
+        "upr_extend_workspace_bytes": (SZ, [VP, pagedp, segp, VP]),
+        "upr_extend_user": (I32, [VP, pagedp, VP, segp, VP, ropep, VP, SZ, VP]),
+        "upr_rank_paged_workspace_bytes": (SZ, [VP, pagedp, segp, VP]),
+        "upr_rank_candidates_paged": (I32, [VP, pagedp, VP, VP, segp, ropep, VP, VP, SZ, VP]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -397,6 +438,218 @@ def current_stream() -> int:
     return int(torch.cuda.current_stream().cuda_stream)
 
 
+# ---------------------------------------------------------------------------
+# Paged K/V cache: rotary positions, append, attention
+# ---------------------------------------------------------------------------
+
+def _check_here(t, name):
+    """The library launches on the current device: tensors live there too."""
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a GPU tensor")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _paged_dtype(t, name) -> int:
+    code = {"torch.float32": UPR_F32, "torch.bfloat16": UPR_BF16}.get(str(t.dtype))
+    if code is None:
+        raise TypeError(f"{name} must be float32 or bfloat16, got {t.dtype}")
+    return code
+
+
+def _rows3(t, name, like=None, heads=None, dim=None, rows=None):
+    """Pointer and leading dimension of t [rows, heads, head_dim], heads one
+    after the other; rows may be strided."""
+    _check_here(t, name)
+    if t.dim() != 3:
+        raise ValueError(f"{name} must be [rows, heads, head_dim]")
+    if like is not None and t.dtype != like:
+        raise TypeError(f"{name} must be {like}, got {t.dtype}")
+    if (heads is not None and t.shape[1] != heads) or (dim is not None and t.shape[2] != dim):
+        raise ValueError(f"{name} has {t.shape[1]} heads of {t.shape[2]}, expected {heads} of {dim}")
+    if rows is not None and t.shape[0] < rows:
+        raise ValueError(f"{name} has {t.shape[0]} rows, {rows} needed")
+    if t.shape[0] > 0 and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2])):
+        raise ValueError(f"{name} must hold each row's heads one after the other")
+    ld = t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1] * t.shape[2])
+    return t.data_ptr(), ld
+
+
+def _host_rows(rows_host, users):
+    if not isinstance(rows_host, np.ndarray) or rows_host.dtype != np.int32 or not rows_host.flags["C_CONTIGUOUS"]:
+        raise TypeError("rows_host must be a contiguous int32 numpy array")
+    if rows_host.shape != (users,):
+        raise ValueError(f"rows_host must have one entry per user ({users})")
+    return rows_host.ctypes.data
+
+
+def _stream_workspace(nbytes: int, stream):
+    """A workspace for a call on `stream` (None: the current one)."""
+    import torch
+    ws = torch.empty(max(nbytes, 256), dtype=torch.uint8, device="cuda")
+    if stream is not None and stream != current_stream():
+        ws.record_stream(torch.cuda.ExternalStream(stream))
+    return ws
+
+
+def rope(rot_dim: int, base: float = 10000.0, layout: str = "half", scaling: str = "none", factor: float = 1.0,
+         original_length: float = 0.0) -> upr_rope:
+    """Rotary positions (upr_rope_init): layout "half" or "interleaved", scaling
+    "none", "linear", "ntk" or "by_parts"."""
+    layouts = {"half": UPR_ROPE_HALF, "interleaved": UPR_ROPE_INTERLEAVED}
+    kinds = {"none": UPR_ROPE_PLAIN, "linear": UPR_ROPE_LINEAR, "ntk": UPR_ROPE_NTK, "by_parts": UPR_ROPE_BY_PARTS}
+    if layout not in layouts or scaling not in kinds:
+        raise ValueError(f"layout must be one of {sorted(layouts)}, scaling one of {sorted(kinds)}")
+    out = upr_rope()
+    _check(load().upr_rope_init(rot_dim, layouts[layout], base, kinds[scaling], factor, original_length,
+                                ctypes.byref(out)))
+    return out
+
+
+def rope_apply(x, positions, rope: upr_rope, out=None, stream=None):
+    """x [rows, heads, head_dim] rotated, row r at positions[r] (int32), into out
+    (a new tensor without one; x itself for in place)."""
+    import torch
+    px, ldx = _rows3(x, "x")
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    po, ldo = _rows3(out, "out", x.dtype, x.shape[1], x.shape[2])
+    if out.shape[0] != x.shape[0]:
+        raise ValueError("out must have x's shape")
+    _check_here(positions, "positions")
+    _check_tensor(positions, "positions", "int32")
+    if tuple(positions.shape) != (x.shape[0],):
+        raise ValueError("positions must be [rows]")
+    _check(load().upr_rope_apply(ctypes.byref(rope), _paged_dtype(x, "x"), x.shape[1], x.shape[2], px, ldx,
+                                 positions.data_ptr(), x.shape[0], po, ldo,
+                                 current_stream() if stream is None else stream))
+    return out
+
+
+class PagedCache:
+    """Users' histories in pages: data [n_pages, 2, kv_heads, page_rows,
+    head_dim] (with n_layers in front for the model calls) and each user's page
+    numbers, tables [users, pages] int32, row p of user u in page
+    tables[u, p // page_rows]."""
+
+    def __init__(self, data, tables):
+        _check_here(data, "data")
+        _check_here(tables, "tables")
+        _paged_dtype(data, "data")
+        if data.dim() not in (5, 6) or data.shape[-4] != 2 or not data.is_contiguous():
+            raise ValueError("data must be a contiguous [n_pages, 2, kv_heads, page_rows, head_dim], or "
+                             "[n_layers, ...] of it")
+        _check_tensor(tables, "tables", "int32")
+        if tables.dim() != 2:
+            raise ValueError("tables must be [users, pages]")
+        self.data, self.tables = data, tables
+
+    @classmethod
+    def for_model(cls, model: "Model", n_pages: int, page_rows: int, tables) -> "PagedCache":
+        import torch
+        c = model.cfg
+        dt = torch.float32 if c.dtype == UPR_F32 else torch.bfloat16
+        data = torch.zeros((c.n_layers, n_pages, 2, c.n_heads, page_rows, c.head_dim), dtype=dt, device="cuda")
+        assert data.numel() * data.element_size() == upr_paged_cache_bytes(c, n_pages, page_rows)
+        return cls(data, tables)
+
+    def view(self, users: int, layer=None) -> upr_paged_cache:
+        """The C struct, of one layer's plane or (None) of the whole pool."""
+        if self.tables.shape[0] < users:
+            raise ValueError(f"tables has {self.tables.shape[0]} users, {users} needed")
+        data = self.data
+        if layer is not None and data.dim() == 6:
+            data = data[layer]
+        elif layer:
+            raise ValueError("the cache has one plane")
+        return upr_paged_cache(data.data_ptr(), data.shape[-5], data.shape[-2], self.tables.shape[1],
+                               self.tables.data_ptr())
+
+    def shape(self, n_heads: int) -> upr_attn_shape:
+        return upr_attn_shape(_paged_dtype(self.data, "data"), n_heads, self.data.shape[-3], self.data.shape[-1])
+
+
+def upr_paged_cache_bytes(cfg: upr_config, n_pages: int, page_rows: int) -> int:
+    return int(load().upr_paged_cache_bytes(ctypes.byref(cfg), n_pages, page_rows))
+
+
+def paged_append(cache: PagedCache, off_host, rows_host, k, v, rope=None, q=None, q_out=None, layer: int = 0,
+                 stream=None) -> None:
+    """upr_paged_append on tensors: k and v [rows, kv_heads, head_dim], q and
+    q_out [rows, heads, head_dim]; off_host the users' rows, rows_host the rows
+    cached when the call ends."""
+    seg = segments(off_host)
+    rows = int(off_host[-1])
+    H, D, dt = cache.data.shape[-3], cache.data.shape[-1], cache.data.dtype
+    pk, ldk = _rows3(k, "k", dt, H, D, rows)
+    pv, ldv = _rows3(v, "v", dt, H, D, rows)
+    n_heads, pq, ldq, po, ldo = H, None, 0, None, 0
+    if q is not None:
+        n_heads = q.shape[1]
+        pq, ldq = _rows3(q, "q", dt, None, D, rows)
+    if q_out is not None:
+        po, ldo = _rows3(q_out, "q_out", dt, n_heads, D, rows)
+    _check(load().upr_paged_append(ctypes.byref(cache.shape(n_heads)), ctypes.byref(cache.view(seg.num_users, layer)),
+                                   ctypes.byref(seg), _host_rows(rows_host, seg.num_users),
+                                   None if rope is None else ctypes.byref(rope), pk, ldk, pv, ldv, pq, ldq, po, ldo,
+                                   current_stream() if stream is None else stream))
+
+
+def _attn_options(scale, softcap, window, slopes, head_dim, k_self=0, v_self=0, self_ld=0) -> upr_attn_options:
+    return upr_attn_options(head_dim ** -0.5 if scale is None else scale, softcap, window,
+                            0 if slopes is None else slopes.data_ptr(), k_self, v_self, self_ld)
+
+
+def paged_attention_workspace(cache: PagedCache, off_host, rows_host, n_heads: int, window: int = 0,
+                              own_keys: bool = False, stream=None):
+    """Workspace for upr_paged_attention calls of these lengths."""
+    seg = segments(off_host)
+    flag = 16 if own_keys else 0            # (not read, only whether it is given)
+    opt = _attn_options(None, 0.0, window, None, cache.data.shape[-1], flag, flag)
+    return _stream_workspace(int(load().upr_paged_attention_workspace_bytes(
+        ctypes.byref(cache.shape(n_heads)), ctypes.byref(cache.view(seg.num_users, 0)), ctypes.byref(seg),
+        _host_rows(rows_host, seg.num_users), ctypes.byref(opt))), stream)
+
+
+def paged_attention(cache: PagedCache, off_host, rows_host, q, out=None, scale=None, softcap: float = 0.0,
+                    window: int = 0, slopes=None, k_self=None, v_self=None, ws=None, layer: int = 0, stream=None):
+    """upr_paged_attention on tensors: q and out [rows, heads, head_dim] (out: a
+    new tensor without one), slopes float32 [heads], k_self and v_self
+    [rows, kv_heads, head_dim] for ranking candidates.  scale: 1 /
+    sqrt(head_dim) by default."""
+    import torch
+    seg = segments(off_host)
+    rows = int(off_host[-1])
+    H, D, dt = cache.data.shape[-3], cache.data.shape[-1], cache.data.dtype
+    pq, ldq = _rows3(q, "q", dt, None, D, rows)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    po, ldo = _rows3(out, "out", dt, q.shape[1], D, rows)
+    if slopes is not None:
+        _check_here(slopes, "slopes")
+        _check_tensor(slopes, "slopes", "float32")
+        if tuple(slopes.shape) != (q.shape[1],):
+            raise ValueError("slopes must be [heads]")
+    pks = pvs = lds = 0
+    if k_self is not None:
+        pks, lds = _rows3(k_self, "k_self", dt, H, D, rows)
+    if v_self is not None:
+        pvs, ldv = _rows3(v_self, "v_self", dt, H, D, rows)
+        if k_self is not None and ldv != lds:
+            raise ValueError("k_self and v_self must have the same row stride")
+    opt = _attn_options(scale, softcap, window, slopes, D, pks, pvs, lds)
+    if ws is None:
+        ws = paged_attention_workspace(cache, off_host, rows_host, q.shape[1], window, k_self is not None, stream)
+    _check_here(ws, "ws")
+    _check_tensor(ws, "ws", "uint8")
+    _check(load().upr_paged_attention(ctypes.byref(cache.shape(q.shape[1])),
+                                      ctypes.byref(cache.view(seg.num_users, layer)), ctypes.byref(seg),
+                                      _host_rows(rows_host, seg.num_users), ctypes.byref(opt), pq, ldq, po, ldo,
+                                      ws.data_ptr(), ws.numel(), current_stream() if stream is None else stream))
+    return out
+
+
 class Model:
     """A created model plus the tensor-level encode/rank calls."""
 
@@ -478,6 +731,52 @@ class Model:
                          0 if probs is None else probs.data_ptr(),
                          0 if utility is None else utility.data_ptr(),
                          ws.data_ptr(), ws.numel(), current_stream() if stream is None else stream)
+        return ws
+
+
+    def _paged_call(self, cache: PagedCache, emb, name, off_host, rows_host):
+        _check_here(emb, name)
+        _check_tensor(emb, name, self.torch_dtype)
+        c = self.cfg
+        want = (c.n_layers, 2, c.n_heads, c.head_dim)
+        d = cache.data
+        if d.dim() != 6 or (d.shape[0], d.shape[2], d.shape[3], d.shape[5]) != want or \
+                str(d.dtype) != f"torch.{self.torch_dtype}":
+            raise ValueError("the cache's pages were not made for this model")
+        seg = segments(off_host)
+        if emb.dim() != 2 or emb.shape[1] != c.d_model or emb.shape[0] < int(off_host[-1]):
+            raise ValueError(f"{name} must be [rows, d_model] with a row for every segment entry")
+        return seg, cache.view(seg.num_users), _host_rows(rows_host, seg.num_users)
+
+    def extend(self, emb, off_host, rows_host, cache: PagedCache, rope=None, ws=None, stream=None):
+        """upr_extend_user on tensors: emb [rows, d_model] holds the users' new
+        actions (rows off_host), rows_host the cached rows when the call ends."""
+        seg, kv, rows = self._paged_call(cache, emb, "emb", off_host, rows_host)
+        lib = load()
+        if ws is None:
+            ws = _stream_workspace(int(lib.upr_extend_workspace_bytes(self.handle, ctypes.byref(kv),
+                                                                      ctypes.byref(seg), rows)), stream)
+        _check(lib.upr_extend_user(self.handle, ctypes.byref(kv), emb.data_ptr(), ctypes.byref(seg), rows,
+                                   None if rope is None else ctypes.byref(rope), ws.data_ptr(), ws.numel(),
+                                   current_stream() if stream is None else stream))
+        return ws
+
+    def rank_paged(self, cache: PagedCache, rows_host, cand_emb, cand_off_host, scores, rope=None, ws=None,
+                   stream=None):
+        """upr_rank_candidates_paged on tensors."""
+        seg, kv, rows = self._paged_call(cache, cand_emb, "cand_emb", cand_off_host, rows_host)
+        _check_here(scores, "scores")
+        _check_tensor(scores, "scores", "float32")
+        if scores.numel() < int(cand_off_host[-1]):
+            raise ValueError("scores must hold one value per candidate row")
+        lib = load()
+        if ws is None:
+            ws = _stream_workspace(int(lib.upr_rank_paged_workspace_bytes(self.handle, ctypes.byref(kv),
+                                                                          ctypes.byref(seg), rows)), stream)
+        _check(lib.upr_rank_candidates_paged(self.handle, ctypes.byref(kv), rows, cand_emb.data_ptr(),
+                                             ctypes.byref(seg), None if rope is None else ctypes.byref(rope),
+                                             scores.data_ptr(), ws.data_ptr(), ws.numel(),
+                                             current_stream() if stream is None else stream))
         return ws
 
 
