@@ -517,8 +517,8 @@ upr_status upr_paged_append(const upr_attn_shape* shape, const upr_paged_cache* 
  * keys that the query sees. */
 typedef struct {
     float scale;            /* > 0, below 1e30                              */
-    float softcap;          /* 0: none, or > 0, below 1e30, with a finite
-                             * scale / softcap                              */
+    float softcap;          /* 0: none, or > 0, below 1e30, with
+                             * scale / softcap below 1e30                   */
     int32_t window;         /* > 0: only the last `window` positions up to
                              * the query's own, itself included; 0: all     */
     const float* slopes;

@@ -1,6 +1,31 @@
-// Attention of new rows over a paged cache, one wave per (row, query head):
-// lanes take keys 64 at a time for the scores and features for the weighted
-// values; running maximum, sum and output in fp32.
+// Attention of new rows over a paged cache on the matrix cores.
+//
+// Rows are (token, query head of one key/value head's group) pairs, so shared
+// K/V heads are read once for all their query heads.  One workgroup = one work
+// item: a tile of rows of one (user, key/value head), over all keys the tile
+// sees or, where a call has few rows, over one part of them.  Its waves are RW
+// groups of 16 QG rows times KW groups of keys: many rows share each K/V stage
+// (RW), or the four waves of one 16- or 32-row tile take different keys of the
+// stage (KW).  K/V stages go straight from the pages to LDS (buffer loads that
+// return zeros past the user's rows and for page numbers outside the pool;
+// double-buffered).  Per 32 keys (16 in fp32) a wave computes
+//   S^T = K Q^T,   P = 2^(z - m),   O^T += V^T P^T
+// with z the scaled (capped, biased, masked) score in log2 units: a lane holds
+// scores of one row, and its packed probabilities are the next product's
+// operand as they stand.  bf16: v_mfma_f32_16x16x32_bf16, bf16 probabilities
+// (one rounding, 2^-8; the row sum adds the rounded values); V^T by transposing
+// LDS reads.  fp32: v_mfma_f32_16x16x4_f32, everything fp32.
+//
+// The running reference m follows a row's maximum only when a score passes it
+// by 2^kSlack: probabilities then reach 2^kSlack instead of 1, which costs no
+// precision, and O is rescaled a few times per row instead of every block.  A
+// row's decision uses its own scores only, so its result does not depend on
+// the rows beside it.
+//
+// Key groups are merged through LDS, key parts by k_paged_attn_join from the
+// workspace.  A row whose result is not finite (a masked key's NaN or infinite
+// value times probability 0, or scores beyond the reference's range) is done
+// again by attn_row, which touches visible keys only.
 #include <type_traits>
 
 #include "upr_paged.h"
@@ -8,6 +33,16 @@
 namespace upr {
 
 namespace {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 b8;
+typedef __attribute__((ext_vector_type(4))) __bf16 b4;
+typedef __attribute__((ext_vector_type(2))) __bf16 b2;
+typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 b4v;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) _Float16 h4;
+
+constexpr float kUnset = -1e30f;        // reference of a row that has seen no key
+constexpr float kSlack = 8.0f;
 
 __device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
@@ -19,30 +54,77 @@ __device__ __forceinline__ float wave_sum(float v) {
     for (int x = 32; x >= 1; x >>= 1) v += __shfl_xor(v, x, 64);
     return v;
 }
+// Over the four lanes {l, l^16, l^32, l^48} of one row.
+__device__ __forceinline__ float quad_max(float v) {
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float quad_sum(float v) {
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
 
-// Score in log2 units.
+// 2^x on the transcendental unit (below 2^-126: 0).
+__device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+
+__device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
+
+// Score in log2 units.  tanh x = 1 - 2 / (2^(2 x log2 e) + 1), off by about
+// 2^-23: the cap is far above any difference of scores that matters.
 __device__ __forceinline__ float score2(const AttnArgs& a, float dot, float slope2, int away) {
-    float z = a.cap2 > 0.f ? a.cap2 * tanhf(dot * a.ct) : dot * a.c;
+    float z = dot * a.c;
+    if (a.cap2 > 0.f) {
+        const float t = fast_exp2(dot * a.ct2);
+        z = a.cap2 * fmaf(-2.f, __builtin_amdgcn_rcpf(t + 1.f), 1.f);
+    }
     return fmaf(slope2, (float)away, z);
 }
 
-template <typename T, int D>
-__global__ __launch_bounds__(256) void k_paged_attn_row(AttnArgs a, PagedPool pool, PagedUsers users) {
-    int lo = 0, hi = users.n - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (users.item0[mid] <= (int)blockIdx.x) lo = mid; else hi = mid - 1;
-    }
+// Where an item stands.
+struct Item {
+    int user;               // row of the page table
+    int64_t row0;           // first row of the user's q / out
+    int count, rows;        // new rows, cached rows
+    int kh, tile, split, splits;
+};
+
+template <int TR>
+__device__ __forceinline__ Item find_item(const AttnArgs& a, const PagedUsers& users, int b) {
+    // the last user whose items start at or before b
     const int lane = threadIdx.x & 63;
-    const int64_t w = (int64_t)((int)blockIdx.x - users.item0[lo]) * 4 + (threadIdx.x >> 6);
-    if (w >= (int64_t)users.count[lo] * a.n_heads) return;
-    const int t = (int)(w / a.n_heads), h = (int)(w % a.n_heads), kh = h / (a.n_heads / a.n_kv_heads);
-    const int64_t row = (int64_t)users.row0[lo] + t;
+    int i = 0;
+#pragma unroll
+    for (int base = 0; base < kPagedUsers; base += 64)
+        i += __popcll(__ballot(base + lane < users.n && users.item0[base + lane + 1] <= b));
+    i = __builtin_amdgcn_readfirstlane(i);
+    Item it;
+    it.user = users.user[i];
+    it.row0 = users.row0[i];
+    it.count = users.count[i];
+    it.rows = users.rows[i];
+    it.splits = attn_splits(it.rows, it.count, a.k_self.p != nullptr, a.window, a.chunk);
+    const int idx = b - users.item0[i], r = idx / a.n_kv_heads;
+    it.kh = idx - r * a.n_kv_heads;
+    it.tile = r / it.splits;
+    it.split = r - it.tile * it.splits;
+    // causal: a user's last tiles see the most keys and go first
+    if (a.k_self.p == nullptr) it.tile = (it.count * (a.n_heads / a.n_kv_heads) + TR - 1) / TR - 1 - it.tile;
+    return it;
+}
+
+// One row by one wave, from its visible keys alone (speed is of no concern).
+template <typename T, int D>
+__device__ __forceinline__ void attn_row(const AttnArgs& a, const PagedPool& pool, int user, int rows, int64_t row,
+                                                   int pos, int h) {
+    const int lane = threadIdx.x & 63, kh = h / (a.n_heads / a.n_kv_heads);
     const bool own = a.k_self.p != nullptr;
-    const int pos = own ? users.rows[lo] : users.rows[lo] - users.count[lo] + t;
-    const int end = own ? pos : pos + 1;                // keys first .. end - 1
+    const int end = own ? rows : pos + 1;               // keys first .. end - 1
     const int first = a.window > 0 && pos - a.window + 1 > 0 ? pos - a.window + 1 : 0;
-    const int32_t* const table = pool.tables + (int64_t)users.user[lo] * pool.stride;
+    const int32_t* const table = pool.tables + (int64_t)user * pool.stride;
     const T* const q = static_cast<const T*>(a.q.p) + row * a.q.ld + (int64_t)h * D;
     const float slope2 = a.slopes != nullptr ? a.slopes[h] * 1.4426950408889634f : 0.f;
     auto place = [&](int j, int kv) -> const T* {       // null: a page outside the pool
@@ -63,11 +145,11 @@ __global__ __launch_bounds__(256) void k_paged_attn_row(AttnArgs a, PagedPool po
     if (own) {
         const T* const vs = static_cast<const T*>(a.v_self.p) + row * a.v_self.ld + (int64_t)kh * D;
         m = score2(a, dot(static_cast<const T*>(a.k_self.p) + row * a.k_self.ld + (int64_t)kh * D), slope2, 0);
-        l = lane == 0 ? 1.f : 0.f;
-        for (int i = 0; i < kE; ++i) acc[i] = (float)vs[i * 64 + lane % D];
-        if (m == -INFINITY) {
-            l = 0.f;
-            for (int i = 0; i < kE; ++i) acc[i] = 0.f;
+        if (m > -INFINITY) {
+            l = lane == 0 ? 1.f : 0.f;
+            for (int i = 0; i < kE; ++i) acc[i] = (float)vs[i * 64 + lane % D];
+        } else if (m != m) {
+            l = m;
         }
     }
     for (int j0 = first; j0 < end; j0 += 64) {
@@ -75,8 +157,8 @@ __global__ __launch_bounds__(256) void k_paged_attn_row(AttnArgs a, PagedPool po
         const float s = lane < n ? score2(a, dot(place(j0 + lane, 0)), slope2, j0 + lane - pos) : -INFINITY;
         const float mn = fmaxf(m, wave_max(s));
         const float ref = mn == -INFINITY ? 0.f : mn;
-        const float alpha = exp2f(m - ref);
-        const float p = lane < n ? exp2f(s - ref) : 0.f;
+        const float alpha = fast_exp2(m - ref);
+        const float p = lane < n ? fast_exp2(s - ref) : 0.f;
         m = mn;
         l = l * alpha + p;
         for (int i = 0; i < kE; ++i) acc[i] *= alpha;
@@ -98,20 +180,532 @@ __global__ __launch_bounds__(256) void k_paged_attn_row(AttnArgs a, PagedPool po
     }
 }
 
+// LDS rows of D values, their 16-byte chunks XOR-swizzled: bf16 K fragments are
+// 16 rows at one chunk, V fragments 8 rows x 32 bytes per pass, and the keys
+// put them on distinct banks (a 256-byte bank period holds 4, 2 or 1 rows).
+// fp32 K fragments likewise; fp32 V rows are read whole.
+template <typename T, int D> __device__ __forceinline__ int key_k(int row) {
+    constexpr int bytes = D * (int)sizeof(T);
+    return bytes == 64 ? (row >> 2) & 3 : bytes == 128 ? (row >> 1) & 7 : row & 15;
+}
+template <typename T, int D> __device__ __forceinline__ int key_v(int row) {
+    if (sizeof(T) == 4) return 0;
+    return D == 32 ? ((row >> 2) & 1) << 1 : D == 64 ? ((row >> 1) & 3) << 1 : (row & 7) << 1;
+}
+
+// Keys of a stage: 8 KB or more of each matrix, a whole block per key group.
+template <typename T, int D, int KW>
+constexpr int stage_keys() {
+    return sizeof(T) == 2 ? (KW == 1 ? (D == 32 ? 128 : 64) : (D == 32 ? 64 : 32) * KW)
+                          : (KW == 1 ? (D == 128 ? 32 : 4096 / D) : D == 128 ? 16 * KW : 4096 / D);
+}
+
+template <typename T, int D, int QG, int RW, int KW, bool EX>
+__global__ __launch_bounds__(64 * RW * KW, 2) void k_paged_attn(AttnArgs a, PagedPool pool, PagedUsers users) {
+    constexpr bool kBf = sizeof(T) == 2;
+    constexpr int NW = RW * KW, SB = kBf ? 32 : 16, NT = SB / 16;
+    constexpr int TS = stage_keys<T, D, KW>(), KS = TS / KW;
+    constexpr int EB = D / 16, ES = kBf ? D / 32 : D / 16;
+    constexpr int CR = D * (int)sizeof(T) / 16, RPL = 64 / CR;     // 16-byte chunks per row, rows per load
+    constexpr int RPW = TS / NW, NI = RPW / RPL, NP = RPW > 16 ? RPW / 16 : 1;
+    constexpr int TR = 16 * QG * RW;
+    static_assert(KS % SB == 0 && RPW % RPL == 0 && NI >= 1 && NI <= 8 && NP <= 4, "stage");
+    __shared__ __attribute__((aligned(16))) T sK0[TS * D];
+    __shared__ __attribute__((aligned(16))) T sK1[TS * D];
+    __shared__ __attribute__((aligned(16))) T sV0[TS * D];
+    __shared__ __attribute__((aligned(16))) T sV1[TS * D];
+
+    const Item it = find_item<TR>(a, users, blockIdx.x);
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int rw = wave % RW, kg = wave / RW;
+    const int g = lane >> 4, l16 = lane & 15;
+    const bool own = a.k_self.p != nullptr;
+    const int G = a.n_heads / a.n_kv_heads;
+    const int n = it.rows, nrows = it.count * G;
+    const int pos0 = own ? n : n - it.count;            // position of the user's first row
+    const int tile0 = it.tile * TR;
+    const int tlast = (tile0 + TR < nrows ? tile0 + TR : nrows) - 1;
+    // keys of the tile, then of this part of them
+    const int end = own ? n : pos0 + tlast / G + 1;
+    const int first = attn_first_key(own ? n : pos0 + tile0 / G, a.window);
+    const int k0 = a.chunk > 0 ? first + it.split * a.chunk : first;
+    const int k1 = a.chunk > 0 && k0 + a.chunk < end ? k0 + a.chunk : end;
+    const int nst = k1 > k0 ? (k1 - k0 + TS - 1) / TS : 0;
+    // this wave's rows
+    const int wrow = tile0 + rw * 16 * QG;
+    const bool active = wrow < nrows;
+    const int wlast = wrow + 16 * QG < nrows ? wrow + 16 * QG - 1 : nrows - 1;
+    const int pfirst = own ? n - 1 : pos0 + wrow / G, plast = own ? n - 1 : pos0 + wlast / G;
+    const int wend = plast + 1;                         // keys from here on: none for the wave
+    // keys below this one are outside the last row's window, from wbeg on inside the first row's
+    const int wlow = a.window > 0 ? (own ? n : plast) - a.window + 1 : 0;
+    const int wbeg = a.window > 0 ? (own ? n : pfirst) - a.window + 1 : 0;
+
+    // ---- K/V stages
+    const int32_t* const table = pool.tables + (int64_t)it.user * pool.stride;
+    const int64_t block = (int64_t)pool.page_rows * D * (int)sizeof(T);     // one head's rows of a page
+    const int rbase = wave * RPW;
+    int offK[8], offV[8];
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+        const int row = rbase + i * RPL + lane / CR, slot = lane % CR;
+        const int r16 = (i * RPL) % 16 + lane / CR;     // row of its 16-row piece (RPW below 16: of the wave's)
+        offK[i] = r16 * D * (int)sizeof(T) + ((slot ^ key_k<T, D>(row)) << 4);
+        offV[i] = r16 * D * (int)sizeof(T) + ((slot ^ key_v<T, D>(row)) << 4);
+    }
+    // page numbers of a stage's pieces (a piece never crosses a page)
+    int pid[4];
+    auto fetch_pages = [&](int st) __attribute__((always_inline)) {
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+            const int key = k0 + st * TS + rbase + 16 * p;
+            pid[p] = table[(key < n ? key : n - 1) >> pool.page_shift];
+        }
+    };
+    auto issue_loads = [&](T* dK, T* dV, int st) __attribute__((always_inline)) {
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+            const int key = k0 + st * TS + rbase + 16 * p;
+            const int base = ((key < n ? key : n - 1) >> pool.page_shift) << pool.page_shift;
+            const int page = __builtin_amdgcn_readfirstlane(pid[p]);
+            // rows of the page that hold keys; none in a page outside the pool
+            int valid = n - base < pool.page_rows ? n - base : pool.page_rows;
+            const bool in = page >= 0 && page < pool.n_pages;
+            valid = in ? valid : 0;
+            char* const pk = pool.data + ((int64_t)(in ? page : 0) * 2 * a.n_kv_heads + it.kh) * block;
+            const __amdgpu_buffer_rsrc_t rsK =
+                __builtin_amdgcn_make_buffer_rsrc(pk, (short)0, valid * D * (int)sizeof(T), 0x00020000);
+            const __amdgpu_buffer_rsrc_t rsV = __builtin_amdgcn_make_buffer_rsrc(
+                pk + a.n_kv_heads * block, (short)0, valid * D * (int)sizeof(T), 0x00020000);
+            const int off = (key - base) * D * (int)sizeof(T);
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                if (i * RPL / 16 != p) continue;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                    rsK, (__attribute__((address_space(3))) void*)(dK + (rbase + i * RPL) * D), 16, offK[i] + off, 0, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                    rsV, (__attribute__((address_space(3))) void*)(dV + (rbase + i * RPL) * D), 16, offV[i] + off, 0, 0, 0);
+            }
+        }
+    };
+    if (nst > 0) {
+        fetch_pages(0);
+        issue_loads(sK0, sV0, 0);
+        if (nst > 1) fetch_pages(1);
+    }
+
+    // ---- the lane's rows
+    typedef std::conditional_t<kBf, b8, f32x4> frag;
+    frag qf[QG][ES];
+    f32x4 o[QG][EB];            // bf16: e = 16 eb + 4g + r; fp32: e = EB (4g + r) + eb
+    float l[QG], negm[QG], slope2[QG];
+    int rpos[QG], low[QG], seen[QG];
+#pragma unroll
+    for (int qg = 0; qg < QG; ++qg) {
+        int r = wrow + qg * 16 + l16;
+        r = r < nrows ? r : nrows - 1;                  // (a ragged tail repeats the last row)
+        const int t = r / G, h = it.kh * G + (r - t * G);
+        const int64_t row = it.row0 + t;
+        rpos[qg] = pos0 + (own ? 0 : t);
+        low[qg] = a.window > 0 && rpos[qg] >= a.window ? rpos[qg] - a.window + 1 : 0;
+        const int high = own || rpos[qg] + 1 > k1 ? k1 : rpos[qg] + 1;
+        seen[qg] = high > low[qg] ? high - low[qg] : 0;
+        if constexpr (EX) slope2[qg] = a.slopes != nullptr ? a.slopes[h] * 1.4426950408889634f : 0.f;
+        const T* const qrow = static_cast<const T*>(a.q.p) + row * a.q.ld + (int64_t)h * D;
+#pragma unroll
+        for (int es = 0; es < ES; ++es)
+            qf[qg][es] = *reinterpret_cast<const frag*>(qrow + (kBf ? es * 32 + 8 * g : (4 * es + g) * 4));
+        l[qg] = 0.f;
+        negm[qg] = -kUnset;
+#pragma unroll
+        for (int eb = 0; eb < EB; ++eb) o[qg][eb] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (own && kg == 0 && it.split == 0) {          // starts from the row's own key
+            const T* const krow = static_cast<const T*>(a.k_self.p) + row * a.k_self.ld + (int64_t)it.kh * D;
+            const T* const vrow = static_cast<const T*>(a.v_self.p) + row * a.v_self.ld + (int64_t)it.kh * D;
+            float s = 0.f;
+#pragma unroll
+            for (int es = 0; es < ES; ++es) {
+                const frag kf = *reinterpret_cast<const frag*>(krow + (kBf ? es * 32 + 8 * g : (4 * es + g) * 4));
+#pragma unroll
+                for (int j = 0; j < (kBf ? 8 : 4); ++j) s = fmaf((float)qf[qg][es][j], (float)kf[j], s);
+            }
+            const float z = score2(a, quad_sum(s), 0.f, 0);
+            if (z > kUnset) {                           // (else: attn_row, as for any row out of range)
+                negm[qg] = -z;
+                l[qg] = g == 0 ? 1.f : 0.f;
+            } else {
+                l[qg] = NAN;
+            }
+#pragma unroll
+            for (int eb = 0; eb < EB; ++eb)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[qg][eb][r] = (float)vrow[kBf ? 16 * eb + 4 * g + r : EB * (4 * g + r) + eb];
+        }
+    }
+
+    // ---- one block of SB keys: rows kb .. of the stage, keys kabs .. of the user
+    auto sub_block = [&](const T* cK, const T* cV, int kb, int kabs) __attribute__((always_inline)) {
+        f32x4 s[QG][NT];
+        if constexpr (kBf) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                b8 kf[ES];
+                const int row = kb + t * 16 + l16;
+#pragma unroll
+                for (int es = 0; es < ES; ++es)
+                    kf[es] = *reinterpret_cast<const b8*>(&cK[row * D + (((es * 4 + g) ^ key_k<T, D>(row)) << 3)]);
+#pragma unroll
+                for (int qg = 0; qg < QG; ++qg) {
+                    s[qg][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int es = 0; es < ES; ++es)
+                        s[qg][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[es], qf[qg][es], s[qg][t], 0, 0, 0);
+                }
+            }
+            mfma_settled<8>();
+        } else {
+            f32x4 so[QG];               // two chains: half the rounding error of one
+#pragma unroll
+            for (int qg = 0; qg < QG; ++qg) s[qg][0] = so[qg] = f32x4{0.f, 0.f, 0.f, 0.f};
+            const int row = kb + l16;
+#pragma unroll
+            for (int es = 0; es < ES; ++es) {
+                const f32x4 kf = *reinterpret_cast<const f32x4*>(cK + row * D + (((4 * es + g) ^ key_k<T, D>(row)) << 2));
+#pragma unroll
+                for (int qg = 0; qg < QG; ++qg)
+#pragma unroll
+                    for (int i = 0; i < 4; i += 2) {
+                        s[qg][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[i], qf[qg][es][i], s[qg][0], 0, 0, 0);
+                        so[qg] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[i + 1], qf[qg][es][i + 1], so[qg], 0, 0, 0);
+                    }
+            }
+            mfma_settled<16>();
+#pragma unroll
+            for (int qg = 0; qg < QG; ++qg) s[qg][0] += so[qg];
+        }
+        if constexpr (EX) {
+#pragma unroll
+            for (int qg = 0; qg < QG; ++qg)
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        s[qg][t][r] = score2(a, s[qg][t][r], slope2[qg], kabs + t * 16 + 4 * g + r - rpos[qg]);
+        }
+        const float c = EX ? 1.f : a.c;
+        // keys after a row, past the cache, or behind its window
+        if (__builtin_expect(kabs + SB > pfirst + 1 || kabs + SB > k1 || kabs < wlow, 0)) {
+#pragma unroll
+            for (int qg = 0; qg < QG; ++qg)
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        // keys seen: low .. low + seen - 1
+                        if ((unsigned)(kabs + t * 16 + 4 * g + r - low[qg]) >= (unsigned)seen[qg]) s[qg][t][r] = -INFINITY;
+                    }
+        }
+        // references that are passed by too much
+        float top[QG];
+        bool passed = false;
+#pragma unroll
+        for (int qg = 0; qg < QG; ++qg) {
+            float x = fmaxf(fmaxf(s[qg][0][0], s[qg][0][1]), fmaxf(s[qg][0][2], s[qg][0][3]));
+            if constexpr (NT == 2)
+                x = fmaxf(x, fmaxf(fmaxf(s[qg][NT - 1][0], s[qg][NT - 1][1]), fmaxf(s[qg][NT - 1][2], s[qg][NT - 1][3])));
+            top[qg] = x;
+            passed |= fmaf(x, c, negm[qg]) > kSlack;
+        }
+        if (__any(passed)) {
+#pragma unroll
+            for (int qg = 0; qg < QG; ++qg) {
+                const float z = quad_max(top[qg]) * c;
+                const float nm = z + negm[qg] > kSlack ? -z : negm[qg];
+                const float alpha = fast_exp2(nm - negm[qg]);
+                negm[qg] = nm;
+                l[qg] *= alpha;
+#pragma unroll
+                for (int eb = 0; eb < EB; ++eb)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o[qg][eb][r] *= alpha;
+            }
+        }
+        if constexpr (kBf) {
+            b8 pf[QG];
+#pragma unroll
+            for (int qg = 0; qg < QG; ++qg) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) pf[qg][t * 4 + r] = (__bf16)fast_exp2(fmaf(s[qg][t][r], c, negm[qg]));
+                const b2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const b2 pp = {pf[qg][2 * j], pf[qg][2 * j + 1]};
+                    l[qg] = __builtin_amdgcn_fdot2_f32_bf16(pp, ones, l[qg], false);
+                }
+            }
+#pragma unroll
+            for (int eb = 0; eb < EB; ++eb) {
+                b8 vf;
+#pragma unroll
+                for (int hh = 0; hh < 2; ++hh) {
+                    const int row = kb + 16 * hh + 4 * g + (l16 >> 2);
+                    const int ch = 2 * eb + ((l16 & 3) >> 1);
+                    const T* p = &cV[row * D + ((ch ^ key_v<T, D>(row)) << 3) + ((l16 & 1) << 2)];
+                    const b4v v4 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) b4v*)(p));
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) vf[4 * hh + j] = v4[j];
+                }
+#pragma unroll
+                for (int qg = 0; qg < QG; ++qg)
+                    o[qg][eb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[qg], o[qg][eb], 0, 0, 0);
+            }
+        } else {
+            float p[QG][4];
+#pragma unroll
+            for (int qg = 0; qg < QG; ++qg) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) p[qg][r] = fast_exp2(fmaf(s[qg][0][r], c, negm[qg]));
+                l[qg] += (p[qg][0] + p[qg][1]) + (p[qg][2] + p[qg][3]);
+            }
+            constexpr int VW = EB < 4 ? EB : 4;         // values per read of a V row
+            typedef __attribute__((ext_vector_type(VW))) float vrow;
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int j0 = 0; j0 < EB; j0 += VW) {
+                    const vrow v = *reinterpret_cast<const vrow*>(cV + (kb + 4 * g + r) * D + EB * l16 + j0);
+#pragma unroll
+                    for (int j = 0; j < VW; ++j)
+#pragma unroll
+                        for (int qg = 0; qg < QG; ++qg)
+                            o[qg][j0 + j] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[j], p[qg][r], o[qg][j0 + j], 0, 0, 0);
+                }
+        }
+        if constexpr (kBf) mfma_settled<8>(); else mfma_settled<16>();
+    };
+
+    auto stage = [&](const T* cK, const T* cV, T* nK, T* nV, int st) __attribute__((always_inline)) {
+        if (st + 1 < nst) {
+            issue_loads(nK, nV, st + 1);
+            if (st + 2 < nst) fetch_pages(st + 2);
+        }
+        if (active) {
+#pragma unroll
+            for (int i = 0; i < KS / SB; ++i) {
+                const int kb = kg * KS + i * SB, kabs = k0 + st * TS + kb;
+                if (kabs < k1 && kabs < wend && kabs + SB > wbeg) sub_block(cK, cV, kb, kabs);
+            }
+        }
+        __builtin_amdgcn_s_waitcnt(0x0F70);     // vmcnt(0): next stage landed
+        __syncthreads();
+    };
+    if (nst > 0) __builtin_amdgcn_s_waitcnt(0x0F70);
+    __syncthreads();
+    int st = 0;
+    for (; st + 2 <= nst; st += 2) {
+        stage(sK0, sV0, sK1, sV1, st);
+        stage(sK1, sV1, sK0, sV0, st + 1);
+    }
+    if (st < nst) stage(sK0, sV0, sK1, sV1, st);
+
+    // ---- key groups meet in LDS (all reads of the stages ended at the last barrier)
+    if constexpr (KW > 1) {
+        constexpr int kWords = QG * (EB * 4 + 2);
+        static_assert(RW * kWords * 64 * 4 <= TS * D * (int)sizeof(T) && KW <= 4, "merge space");
+        float* const x = reinterpret_cast<float*>(kg == 1 ? sK0 : kg == 2 ? sK1 : sV0) + rw * kWords * 64 + lane;
+        if (kg > 0) {
+#pragma unroll
+            for (int qg = 0; qg < QG; ++qg) {
+#pragma unroll
+                for (int eb = 0; eb < EB; ++eb)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) x[(qg * (EB * 4 + 2) + eb * 4 + r) * 64] = o[qg][eb][r];
+                x[(qg * (EB * 4 + 2) + EB * 4) * 64] = negm[qg];
+                x[(qg * (EB * 4 + 2) + EB * 4 + 1) * 64] = l[qg];
+            }
+        }
+        __syncthreads();
+        if (kg > 0) return;
+#pragma unroll
+        for (int w = 1; w < KW; ++w) {
+            const float* const y = reinterpret_cast<const float*>(w == 1 ? sK0 : w == 2 ? sK1 : sV0) + rw * kWords * 64 + lane;
+#pragma unroll
+            for (int qg = 0; qg < QG; ++qg) {
+                const float nw = y[(qg * (EB * 4 + 2) + EB * 4) * 64];
+                const float nm = fminf(negm[qg], nw);
+                const float a0 = fast_exp2(nm - negm[qg]), a1 = fast_exp2(nm - nw);
+                negm[qg] = nm;
+                l[qg] = l[qg] * a0 + y[(qg * (EB * 4 + 2) + EB * 4 + 1) * 64] * a1;
+#pragma unroll
+                for (int eb = 0; eb < EB; ++eb)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        o[qg][eb][r] = o[qg][eb][r] * a0 + y[(qg * (EB * 4 + 2) + eb * 4 + r) * 64] * a1;
+            }
+        }
+    }
+    if (!active) return;
+
+    // ---- out: this part's state, or the normalised rows
+    unsigned long long again = 0;               // rows of the wave to do again
+#pragma unroll
+    for (int qg = 0; qg < QG; ++qg) {
+        const float lt = quad_sum(l[qg]);
+        const int r = wrow + qg * 16 + l16;
+        const bool valid = r < nrows;
+        if (it.splits > 1) {
+            if (!valid) continue;
+            const int64_t rec = (int64_t)blockIdx.x * TR + (r - tile0);
+            if (g == 0) {
+                a.part_ml[2 * rec] = negm[qg];
+                a.part_ml[2 * rec + 1] = lt;
+            }
+            float* const po = a.part_o + rec * D;
+            if constexpr (kBf) {
+#pragma unroll
+                for (int eb = 0; eb < EB; ++eb) *reinterpret_cast<f32x4*>(po + 16 * eb + 4 * g) = o[qg][eb];
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int eb = 0; eb < EB; ++eb) po[EB * (4 * g + i) + eb] = o[qg][eb][i];
+            }
+            continue;
+        }
+        const float inv = 1.0f / lt;
+        bool bad = !finite(inv) || !(inv > 0.f);
+#pragma unroll
+        for (int eb = 0; eb < EB; ++eb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                o[qg][eb][i] = keep_f32(o[qg][eb][i] * inv);
+                bad |= !finite(o[qg][eb][i]);
+            }
+        const int t = r / G, h = it.kh * G + (r - t * G);
+        const int64_t at = (it.row0 + t) * a.out_ld + (int64_t)h * D;
+        if (valid) {
+            if constexpr (kBf) {
+#pragma unroll
+                for (int eb = 0; eb < EB; ++eb) {
+                    const int64_t e = at + 16 * eb + 4 * g;
+                    const f32x4 v = o[qg][eb];
+                    if (a.out_kind == ATTN_OUT_F32)
+                        *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + e) = v;
+                    else if (a.out_kind == ATTN_OUT_F16)
+                        *reinterpret_cast<h4*>(static_cast<f16*>(a.out) + e) = h4{(f16)v[0], (f16)v[1], (f16)v[2], (f16)v[3]};
+                    else
+                        *reinterpret_cast<b4*>(static_cast<bf16*>(a.out) + e) =
+                            b4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
+                }
+            } else {
+                constexpr int VW = EB < 4 ? EB : 4;
+                typedef __attribute__((ext_vector_type(VW))) float vrow;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j0 = 0; j0 < EB; j0 += VW) {
+                        vrow v;
+#pragma unroll
+                        for (int j = 0; j < VW; ++j) v[j] = o[qg][j0 + j][i];
+                        *reinterpret_cast<vrow*>(static_cast<float*>(a.out) + at + EB * (4 * g + i) + j0) = v;
+                    }
+            }
+        }
+        unsigned long long any = __ballot(bad && valid);
+        any |= any >> 32;
+        again |= ((any | any >> 16) & 0xffff) << (16 * qg);
+    }
+    while (again != 0) {
+        const int ri = wrow + __ffsll((long long)again) - 1, ti = ri / G;
+        again &= again - 1;
+        attn_row<T, D>(a, pool, it.user, n, it.row0 + ti, own ? n : pos0 + ti, it.kh * G + (ri - ti * G));
+    }
+}
+
+// Joins the parts of the rows whose keys were split: one wave per row.  Part
+// records of item b (its tile and key/value head, part 0) follow those of the
+// next part n_kv_heads items on.
+template <typename T, int D, int TR>
+__global__ __launch_bounds__(256) void k_paged_attn_join(AttnArgs a, PagedPool pool, PagedUsers users) {
+    const Item it = find_item<TR>(a, users, blockIdx.x);
+    if (it.splits == 1 || it.split != 0) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int G = a.n_heads / a.n_kv_heads, nrows = it.count * G, tile0 = it.tile * TR;
+    const int here = nrows - tile0 < TR ? nrows - tile0 : TR;
+    constexpr int kE = D > 64 ? D / 64 : 1;
+    for (int i = wave; i < here; i += 4) {
+        auto rec = [&](int s) { return ((int64_t)blockIdx.x + (int64_t)s * a.n_kv_heads) * TR + i; };
+        float nm = -kUnset;
+        for (int s = lane; s < it.splits; s += 64) nm = fminf(nm, a.part_ml[2 * rec(s)]);
+        nm = -wave_max(-nm);
+        float l = 0.f, acc[kE];
+        for (int j = 0; j < kE; ++j) acc[j] = 0.f;
+        for (int s = 0; s < it.splits; ++s) {
+            const int64_t rs = rec(s);
+            const float w = fast_exp2(nm - a.part_ml[2 * rs]);
+            l = fmaf(w, a.part_ml[2 * rs + 1], l);
+#pragma unroll
+            for (int j = 0; j < kE; ++j) acc[j] = fmaf(w, a.part_o[rs * D + j * 64 + lane % D], acc[j]);
+        }
+        const float inv = 1.f / l;
+        bool bad = !finite(inv) || !(inv > 0.f);
+        const int r = tile0 + i, t = r / G, h = it.kh * G + (r - t * G);
+        const int64_t row = it.row0 + t, at = row * a.out_ld + (int64_t)h * D;
+#pragma unroll
+        for (int j = 0; j < kE; ++j) {
+            const float v = keep_f32(acc[j] * inv);
+            bad |= !finite(v);
+            if (lane >= D) continue;
+            if (a.out_kind == ATTN_OUT_F16) static_cast<f16*>(a.out)[at + j * 64 + lane] = (f16)v;
+            else if (a.out_kind == ATTN_OUT_F32) static_cast<float*>(a.out)[at + j * 64 + lane] = v;
+            else static_cast<T*>(a.out)[at + j * 64 + lane] = (T)v;
+        }
+        if (__any(bad))
+            attn_row<T, D>(a, pool, it.user, it.rows, row, a.k_self.p != nullptr ? it.rows : it.rows - it.count + t, h);
+    }
+}
+
+template <typename T, int D, int QG, int RW, int KW>
+hipError_t launch_tiles(const AttnArgs& a, const PagedPool& pool, const PagedUsers& users, bool join, hipStream_t s) {
+    const unsigned grid = (unsigned)users.item0[users.n];
+    if (a.cap2 > 0.f || a.slopes != nullptr)
+        k_paged_attn<T, D, QG, RW, KW, true><<<grid, 64 * RW * KW, 0, s>>>(a, pool, users);
+    else
+        k_paged_attn<T, D, QG, RW, KW, false><<<grid, 64 * RW * KW, 0, s>>>(a, pool, users);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !join) return e;
+    k_paged_attn_join<T, D, 16 * QG * RW><<<grid, 256, 0, s>>>(a, pool, users);
+    return hipGetLastError();
+}
+
+template <typename T, int D>
+hipError_t launch_dim(const AttnArgs& a, const PagedPool& pool, const PagedUsers& users, bool join, hipStream_t s) {
+    constexpr bool bf = sizeof(T) == 2;
+    if (a.tile == 16) return launch_tiles<T, D, 1, 1, 4>(a, pool, users, join, s);
+    if constexpr (bf) {
+        if (a.tile == 32) return launch_tiles<T, D, 2, 1, 4>(a, pool, users, join, s);
+        if (a.tile == 128) return launch_tiles<T, D, 2, 4, 1>(a, pool, users, join, s);
+    } else {
+        if (a.tile == 64) return launch_tiles<T, D, 1, 4, 1>(a, pool, users, join, s);
+    }
+    return hipErrorInvalidValue;
+}
+
 }  // namespace
 
-hipError_t launch_paged_attn(int dtype, const AttnArgs& a, const PagedPool& pool, const PagedUsers& users,
+hipError_t launch_paged_attn(int dtype, const AttnArgs& a, const PagedPool& pool, const PagedUsers& users, bool join,
                              hipStream_t s) {
-    const unsigned grid = (unsigned)users.item0[users.n];
-    if (grid == 0) return hipSuccess;
+    if (users.item0[users.n] == 0) return hipSuccess;
     auto go = [&](auto t) {
         typedef decltype(t) T;
-        if (a.D == 32) k_paged_attn_row<T, 32><<<grid, 256, 0, s>>>(a, pool, users);
-        else if (a.D == 64) k_paged_attn_row<T, 64><<<grid, 256, 0, s>>>(a, pool, users);
-        else k_paged_attn_row<T, 128><<<grid, 256, 0, s>>>(a, pool, users);
+        if (a.D == 32) return launch_dim<T, 32>(a, pool, users, join, s);
+        if (a.D == 64) return launch_dim<T, 64>(a, pool, users, join, s);
+        return launch_dim<T, 128>(a, pool, users, join, s);
     };
-    if (dtype == UPR_F32) go(float{}); else go(bf16{});
-    return hipGetLastError();
+    return dtype == UPR_F32 ? go(float{}) : go(bf16{});
 }
 
 }  // namespace upr

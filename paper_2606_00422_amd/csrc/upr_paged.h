@@ -62,9 +62,22 @@ int64_t append_items(int dtype, const RopeArgs& rope, const AppendArgs& a, int64
 hipError_t launch_append(int dtype, const RopeArgs& rope, const AppendArgs& a, const PagedPool& pool,
                          const PagedUsers& users, hipStream_t s);
 
+// First key that a row at position pos sees, rounded down to a block of keys.
+__host__ __device__ __forceinline__ int attn_first_key(int pos, int window) {
+    return window > 0 && pos - window + 1 > 0 ? (pos - window + 1) & ~31 : 0;
+}
+
+// Parts that a user's keys are cut into (chunk 0: none are).
+__host__ __device__ __forceinline__ int attn_splits(int rows, int count, bool own, int window, int chunk) {
+    if (chunk == 0) return 1;
+    const int keys = rows - attn_first_key(own ? rows : rows - count, window);
+    return keys > chunk ? (keys + chunk - 1) / chunk : 1;
+}
+
 // Attention of one launch's users.  Scores in log2 units: z2 = c (q.k) with c
-// = scale log2(e), or with a cap cap2 tanh(ct (q.k)), ct = scale / cap and
-// cap2 = cap log2(e); slopes are multiplied by log2(e) in the kernel.
+// = scale log2(e), or with a cap cap2 tanh(q.k scale / cap), cap2 = cap log2(e)
+// and ct2 = 2 log2(e) scale / cap; slopes are multiplied by log2(e) in the
+// kernel.
 enum AttnOut : int { ATTN_OUT_STORAGE = 0, ATTN_OUT_F16 = 1, ATTN_OUT_F32 = 2 };
 struct AttnArgs {
     int n_heads, n_kv_heads, D;
@@ -72,12 +85,16 @@ struct AttnArgs {
     void* out;
     int64_t out_ld;
     int out_kind;                   // AttnOut: the cache's type, or what bf16 models' projections take
-    float c, ct, cap2;              // cap2 0: none
+    float c, ct2, cap2;             // cap2 0: none
     const float* slopes;
     int32_t window;                 // 0: none
+    // the plan: rows per tile, keys per part (0: all), and with parts their
+    // records, `tile` per work item: [D] sums, and reference and weight sum
+    int32_t tile, chunk;
+    float* part_o;
+    float* part_ml;
 };
-
-hipError_t launch_paged_attn(int dtype, const AttnArgs& a, const PagedPool& pool, const PagedUsers& users,
+hipError_t launch_paged_attn(int dtype, const AttnArgs& a, const PagedPool& pool, const PagedUsers& users, bool join,
                              hipStream_t s);
 
 }  // namespace upr

@@ -1,5 +1,6 @@
 // Host side of the paged-cache operators: argument checks, frequency tables,
 // and the launches of upr_rope_*, upr_paged_append and upr_paged_attention.
+#include <algorithm>
 #include <cmath>
 
 #include "upr_paged_host.h"
@@ -112,8 +113,8 @@ upr_status check_attn_options(const upr_attn_options* o) {
     // (in log2 units, and as the argument of the tanh, they have to be fp32 too)
     if (!(o->scale > 0.f) || !(o->scale < 1e30f))
         return report_error(UPR_ERR_LIMIT, "scale must be positive and below 1e30");
-    if (!(o->softcap >= 0.f) || !(o->softcap < 1e30f) || (o->softcap > 0.f && !std::isfinite(o->scale / o->softcap)))
-        return report_error(UPR_ERR_LIMIT, "softcap must be 0, or positive, below 1e30 and with a finite scale / softcap");
+    if (!(o->softcap >= 0.f) || !(o->softcap < 1e30f) || (o->softcap > 0.f && !(o->scale / o->softcap < 1e30f)))
+        return report_error(UPR_ERR_LIMIT, "softcap must be 0, or positive, below 1e30 and with scale / softcap below 1e30");
     if (o->window < 0) return report_error(UPR_ERR_LIMIT, "window %d < 0", o->window);
     if ((o->k_self == nullptr) != (o->v_self == nullptr))
         return report_error(UPR_ERR_NULL, "k_self and v_self must both be given or both be NULL");
@@ -177,13 +178,89 @@ hipError_t paged_append(int dtype, const RopeArgs& rope, const AppendArgs& a, co
         [&](const PagedUsers& u) { return launch_append(dtype, rope, a, pool, u, s); });
 }
 
-size_t paged_attn_workspace(int, const AttnArgs&, const upr_segments*, const int32_t*) { return 0; }
+// ---- the attention's plan
 
-hipError_t paged_attn(int dtype, const AttnArgs& a, const PagedPool& pool, const upr_segments* seg,
-                      const int32_t* rows_host, void*, hipStream_t s) {
+static int64_t attn_user_items(const AttnArgs& a, int32_t count, int32_t rows) {
+    const int64_t tiles = ((int64_t)count * (a.n_heads / a.n_kv_heads) + a.tile - 1) / a.tile;
+    return tiles * a.n_kv_heads * attn_splits(rows, count, a.k_self.p != nullptr, a.window, a.chunk);
+}
+
+// Tile, parts and workspace of a call, from its lengths alone.
+static size_t plan_attn(int dtype, AttnArgs* a, const upr_segments* seg, const int32_t* rows_host) {
+    const int32_t* const o = seg->offsets_host;
+    const int G = a->n_heads / a->n_kv_heads;
+    int64_t most = 0;
+    auto items_of = [&](int tile, double* keys) {
+        int64_t items = 0;
+        *keys = 0;
+        for (int u = 0; u < seg->num_users; ++u) {
+            const int64_t c = o[u + 1] - o[u];
+            if (c == 0) continue;
+            const int64_t t = (c * G + tile - 1) / tile * a->n_kv_heads;
+            items += t;
+            *keys += (double)t * (rows_host[u] - attn_first_key(a->k_self.p ? rows_host[u] : rows_host[u] - (int)c, a->window));
+        }
+        return items;
+    };
+    for (int u = 0; u < seg->num_users; ++u) most = std::max<int64_t>(most, (int64_t)(o[u + 1] - o[u]) * G);
+    double keys = 0;
+    a->chunk = 0;
+    if (most <= 16) {
+        a->tile = 16;
+    } else if (dtype == UPR_F32) {
+        a->tile = 64;
+    } else {
+        a->tile = 128;
+        if (items_of(128, &keys) < 512) a->tile = 32;
+    }
+    const int64_t items = items_of(a->tile, &keys);
+    if (items > 0 && items < 1024) {
+        // parts of equal length, whole stages, none below 512 keys
+        const double per = keys / 1024;
+        const int64_t chunk = std::max<int64_t>(512, ((int64_t)per + 255) / 256 * 256);
+        a->chunk = (int32_t)std::min<int64_t>(chunk, 1 << 30);
+    }
+    if (a->chunk == 0) return 0;
+    // launches of a call follow one another and use the same records
+    size_t bytes = 0;
+    bool any = false;
+    int64_t here = 0, most_items = 0;
+    int users = 0;
+    for (int u = 0; u < seg->num_users; ++u) {
+        const int32_t c = o[u + 1] - o[u];
+        if (c == 0) continue;
+        if (users == kPagedUsers) users = 0, here = 0;
+        here += attn_user_items(*a, c, rows_host[u]);
+        ++users;
+        any |= attn_splits(rows_host[u], c, a->k_self.p != nullptr, a->window, a->chunk) > 1;
+        most_items = std::max(most_items, here);
+    }
+    if (!any) {
+        a->chunk = 0;
+        return 0;
+    }
+    const size_t recs = (size_t)most_items * a->tile;
+    bytes = (recs * a->D * 4 + 255) / 256 * 256;
+    a->part_ml = reinterpret_cast<float*>(bytes);       // (offset, until the workspace is known)
+    return bytes + recs * 8;
+}
+
+size_t paged_attn_workspace(int dtype, const AttnArgs& args, const upr_segments* seg, const int32_t* rows_host) {
+    AttnArgs a = args;
+    return plan_attn(dtype, &a, seg, rows_host);
+}
+
+hipError_t paged_attn(int dtype, const AttnArgs& args, const PagedPool& pool, const upr_segments* seg,
+                      const int32_t* rows_host, void* ws, hipStream_t s) {
+    AttnArgs a = args;
+    const bool join = plan_attn(dtype, &a, seg, rows_host) > 0;
+    if (join) {
+        a.part_o = static_cast<float*>(ws);
+        a.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) + reinterpret_cast<uintptr_t>(a.part_ml));
+    }
     return each_launch(
-        seg, rows_host, [&](int32_t c, int32_t) { return ((int64_t)c * a.n_heads + 3) / 4; },
-        [&](const PagedUsers& u) { return launch_paged_attn(dtype, a, pool, u, s); });
+        seg, rows_host, [&](int32_t c, int32_t n) { return attn_user_items(a, c, n); },
+        [&](const PagedUsers& u) { return launch_paged_attn(dtype, a, pool, u, join, s); });
 }
 
 }  // namespace upr
@@ -201,7 +278,7 @@ static AttnArgs attn_args(const upr_attn_shape& sh, const upr_attn_options& o) {
     a.v_self = RowsOf{o.v_self, o.self_ld};
     a.c = (float)(o.scale * 1.4426950408889634);
     if (o.softcap > 0.f) {
-        a.ct = (float)((double)o.scale / o.softcap);
+        a.ct2 = (float)(2 * 1.4426950408889634 * (double)o.scale / o.softcap);
         a.cap2 = (float)(o.softcap * 1.4426950408889634);
     }
     a.slopes = o.slopes;

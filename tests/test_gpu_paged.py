@@ -264,6 +264,11 @@ def test_unseen_rows_have_no_influence(kind, value):
     H, D, n, c = 2, 64, 300, 140
     for window in (0, 50):
         pages, off, q, out, _ = run_attend(rng, kind, [c], [n], H, H, D, 16, window=window)
+        # Not bit for bit: a row may be summed in another order.  Two orders of
+        # n = 300 fp32 terms differ by up to 2 n roundings, 2 * 300 * 2^-24 of the
+        # terms' size, so each result is held to the bound of the formula that
+        # counts them (attend), which the unseen row is no part of.
+        want, bound = attend(q.double().cpu().numpy(), *pages.hist[0], np.arange(n - c, n), kind, window=window)
         value = torch.finfo(pages.dt).max if value is None else value
         for j in (n - 1, n - 30, n - 77, 190, 130, 3):
             where = pages.tables[0, j // 16]
@@ -273,9 +278,8 @@ def test_unseen_rows_have_no_influence(kind, value):
             pages.data[where, :, :, j % 16] = held
             pos = np.arange(n - c, n)
             blind = torch.from_numpy((pos < j) | ((pos >= j + window) if window else np.zeros(c, bool))).cuda()
-            # (the same terms, possibly summed another way)
-            diff = (got[blind].double() - out[blind].double()).abs()
-            assert bool((diff <= 4 * EPS[kind] * (out[blind].double().abs() + 1.0)).all()), (window, j)
+            mask = blind.cpu().numpy()
+            assert_close(got[blind], want[mask], bound[mask], f"window {window}, row {j}")
             if value != value:
                 assert bool(torch.isnan(got[~blind]).all()), (window, j)
 
