@@ -28,7 +28,7 @@
 // again by attn_row, which touches visible keys only.
 #include <type_traits>
 
-#include "upr_paged.h"
+#include "paged_dev.h"
 
 namespace upr {
 
@@ -94,13 +94,7 @@ struct Item {
 
 template <int TR>
 __device__ __forceinline__ Item find_item(const AttnArgs& a, const PagedUsers& users, int b) {
-    // the last user whose items start at or before b
-    const int lane = threadIdx.x & 63;
-    int i = 0;
-#pragma unroll
-    for (int base = 0; base < kPagedUsers; base += 64)
-        i += __popcll(__ballot(base + lane < users.n && users.item0[base + lane + 1] <= b));
-    i = __builtin_amdgcn_readfirstlane(i);
+    const int i = user_of(users, b);
     Item it;
     it.user = users.user[i];
     it.row0 = users.row0[i];

@@ -6,8 +6,12 @@
 // for the pairs (a, b) of a head's first rot_dim features.  A thread takes a
 // unit: VEC features and the VEC they are paired with (half layout), or 2 VEC
 // consecutive ones (interleaved pairs, features past rot_dim, values), so both
-// layouts read and write 16-byte pieces where rot_dim allows (VEC 1 otherwise).
-#include "rope.h"
+// layouts read and write 16-byte pieces where rot_dim allows (VEC 1 otherwise),
+// of several heads of its row: the angles are the same for all of them.
+#include <algorithm>
+#include <type_traits>
+
+#include "paged_dev.h"
 
 namespace upr {
 
@@ -20,165 +24,201 @@ struct Chunk {
 template <> struct __attribute__((aligned(16))) Chunk<bf16, 8> { bf16 v[8]; };
 template <> struct __attribute__((aligned(16))) Chunk<float, 4> { float v[4]; };
 
-template <typename T, int VEC>
-__device__ __forceinline__ void load(const T* p, float (&x)[VEC]) {
-    const Chunk<T, VEC> c = *reinterpret_cast<const Chunk<T, VEC>*>(p);
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) x[i] = (float)c.v[i];
-}
-template <typename T, int VEC>
-__device__ __forceinline__ void store(T* p, const float (&x)[VEC]) {
-    Chunk<T, VEC> c;
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) c.v[i] = (T)keep_f32(x[i]);
-    *reinterpret_cast<Chunk<T, VEC>*>(p) = c;
-}
+// The same pieces as plain bits.
+typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
+template <int BYTES>
+using Raw = std::conditional_t<BYTES == 16, u32x4, std::conditional_t<BYTES == 4, unsigned, unsigned short>>;
 
-// Unit u of one head at position pos (rot: the head is rotated at all).
-template <typename T, int VEC>
-__device__ __forceinline__ void turn_unit(const RopeArgs& rope, bool rot, int u, int pos, const T* x, T* out) {
-    const int r = rot ? rope.rot_dim : 0;
-    const bool turned = 2 * u * VEC < r;
-    const bool half = turned && rope.layout == UPR_ROPE_HALF;
-    const int ia = half ? u * VEC : 2 * u * VEC, ib = half ? ia + r / 2 : ia + VEC;
-    float a[VEC], b[VEC];
-    load<T, VEC>(x + ia, a);
-    load<T, VEC>(x + ib, b);
-    if (half) {
+// A thread's unit of some heads at one position: where its two pieces stand,
+// and the cosines and sines of its VEC pairs.
+template <int VEC>
+struct Unit {
+    int ia, ib;
+    bool turned, half;
+    float c[VEC], s[VEC];
+
+    __device__ __forceinline__ Unit(const RopeArgs& rope, int u, int pos) {
+        turned = 2 * u * VEC < rope.rot_dim;
+        half = turned && rope.layout == UPR_ROPE_HALF;
+        ia = half ? u * VEC : 2 * u * VEC;
+        ib = half ? ia + rope.rot_dim / 2 : ia + VEC;
+        if (!turned) return;
+        // either way its pairs are u VEC .. u VEC + VEC - 1
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-            float c, s;
-            rope_angle(pos, rope.quarters[ia + j], rope.magnitude, c, s);
-            const float xa = a[j], xb = b[j];
-            a[j] = fmaf(xa, c, -(xb * s));
-            b[j] = fmaf(xb, c, xa * s);
-        }
-    } else if (turned) {
-        if constexpr (VEC == 1) {
-            float c, s;
-            rope_angle(pos, rope.quarters[u], rope.magnitude, c, s);
-            const float xa = a[0], xb = b[0];
-            a[0] = fmaf(xa, c, -(xb * s));
-            b[0] = fmaf(xb, c, xa * s);
-        } else {
+        for (int j = 0; j < VEC; ++j) rope_angle(pos, rope.quarters[u * VEC + j], rope.magnitude, c[j], s[j]);
+    }
+    // The unit's two pieces turned (copied bit for bit where it is not).
+    template <typename T>
+    __device__ __forceinline__ void turn(Chunk<T, VEC>& a, Chunk<T, VEC>& b) const {
+        auto pair = [&](T& x, T& y, int j) {
+            const float xa = (float)x, xb = (float)y;
+            x = (T)keep_f32(fmaf(xa, c[j], -(xb * s[j])));
+            y = (T)keep_f32(fmaf(xb, c[j], xa * s[j]));
+        };
+        if (half || (VEC == 1 && turned)) {
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                float(&w)[VEC] = j < VEC / 2 ? a : b;
-                const int k = 2 * (j % (VEC / 2));
-                float c, s;
-                rope_angle(pos, rope.quarters[ia / 2 + j], rope.magnitude, c, s);
-                const float xa = w[k], xb = w[k + 1];
-                w[k] = fmaf(xa, c, -(xb * s));
-                w[k + 1] = fmaf(xb, c, xa * s);
+            for (int j = 0; j < VEC; ++j) pair(a.v[j], b.v[j], j);
+        } else if (turned) {
+            if constexpr (VEC > 1) {
+#pragma unroll
+                for (int j = 0; j < VEC / 2; ++j) {
+                    pair(a.v[2 * j], a.v[2 * j + 1], j);
+                    pair(b.v[2 * j], b.v[2 * j + 1], VEC / 2 + j);
+                }
             }
         }
     }
-    store<T, VEC>(out + ia, a);
-    store<T, VEC>(out + ib, b);
+};
+
+// Heads h0, h0 + step, .. of one row, kBatch at a time: all of a batch's loads
+// are under way before its first store.
+template <typename T, int VEC, int kBatch, bool TURN>
+__device__ __forceinline__ void row_heads(const Unit<VEC>& unit, int h0, int step, int heads, int64_t x_step,
+                                          int64_t out_step, const T* x, T* out) {
+    for (int h = h0; h < heads; h += kBatch * step) {
+        typedef std::conditional_t<TURN, Chunk<T, VEC>, Raw<VEC * sizeof(T)>> C;
+        C a[kBatch], b[kBatch];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            // (past the last head: the last one again, not stored)
+            const T* const p = x + (h + i * step < heads ? h + i * step : heads - 1) * x_step;
+            a[i] = *reinterpret_cast<const C*>(p + unit.ia);
+            b[i] = *reinterpret_cast<const C*>(p + unit.ib);
+        }
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            if constexpr (TURN) unit.turn(a[i], b[i]);
+            if (h + i * step < heads) {
+                T* const p = out + (h + i * step) * out_step;
+                *reinterpret_cast<C*>(p + unit.ia) = a[i];
+                *reinterpret_cast<C*>(p + unit.ib) = b[i];
+            }
+        }
+    }
 }
 
-template <typename T, int VEC>
+// A row's threads: `groups` of D / (2 VEC), group j taking heads j, j + groups,
+// ..: `batch` heads of a tensor each (they share the angles and have their
+// loads under way together), as far as a block of 256 threads has groups.
+struct Split {
+    int groups, rows;       // rows per block
+};
+__host__ __device__ __forceinline__ Split split_row(int vec, int batch, int heads, int D) {
+    const int units = D / (2 * vec), most = 256 / units;
+    const int groups = (heads + batch - 1) / batch;
+    Split s;
+    s.groups = groups < most ? groups : most;
+    s.rows = 256 / (s.groups * units);
+    return s;
+}
+
+// Heads per thread: 4 in calls that fill the device many times over, where the
+// memory's rate counts (append of 62,830 rows: 123 us with 1, 80 with 4), else
+// 1 (64 rows: 5.9 us with 1, 11.9 with 4).
+constexpr int64_t kManyThreads = int64_t{1} << 20;
+inline int batch_of(int64_t rows, int heads, int D, int vec) {
+    return rows * heads * (D / (2 * vec)) >= kManyThreads ? 4 : 1;
+}
+
+template <typename T, int VEC, int kBatch>
 __global__ __launch_bounds__(256) void k_rope(RopeArgs rope, int heads, int D, const T* x, int64_t x_ld,
                                               const int32_t* __restrict__ positions, int64_t rows, T* out,
                                               int64_t out_ld) {
-    const int upr_ = heads * (D / (2 * VEC));       // units per row
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= rows * upr_) return;
-    const int64_t row = i / upr_;
-    const int w = (int)(i - row * upr_), h = w / (D / (2 * VEC)), u = w % (D / (2 * VEC));
-    turn_unit<T, VEC>(rope, true, u, positions[row], x + row * x_ld + h * D, out + row * out_ld + h * D);
+    const int units = D / (2 * VEC);
+    const Split sp = split_row(VEC, kBatch, heads, D);
+    const int t = threadIdx.x / (units * sp.groups), rest = threadIdx.x - t * units * sp.groups;
+    const int64_t row = (int64_t)blockIdx.x * sp.rows + t;
+    if (t >= sp.rows || row >= rows) return;
+    const Unit<VEC> unit(rope, rest % units, positions[row]);
+    row_heads<T, VEC, kBatch, true>(unit, rest / units, sp.groups, heads, D, D, x + row * x_ld, out + row * out_ld);
 }
 
-// The launch's user that item b belongs to: the last one whose items start at
-// or before b.
-__device__ __forceinline__ int user_of(const PagedUsers& users, int b) {
-    int lo = 0, hi = users.n - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (users.item0[mid] <= b) lo = mid; else hi = mid - 1;
-    }
-    return lo;
-}
-
-constexpr int kAppendUnits = 256;       // units per work item
-
-template <typename T, int VEC>
+template <typename T, int VEC, int kBatch>
 __global__ __launch_bounds__(256) void k_append(RopeArgs rope, AppendArgs a, PagedPool pool, PagedUsers users) {
     const int i = user_of(users, blockIdx.x);
-    const int per = a.D / (2 * VEC);
+    const int units = a.D / (2 * VEC);
     const int kvh = a.k.p != nullptr ? a.n_kv_heads : 0, qh = a.q.p != nullptr ? a.n_heads : 0;
-    const int heads = 2 * kvh + qh;
-    const int64_t w = (int64_t)((int)blockIdx.x - users.item0[i]) * kAppendUnits + threadIdx.x;
-    if (w >= (int64_t)users.count[i] * heads * per) return;
-    const int t = (int)(w / (heads * per)), rest = (int)(w % (heads * per));
-    const int h = rest / per, u = rest % per;
+    const Split sp = split_row(VEC, kBatch, kvh > qh ? kvh : qh, a.D);
+    const int tr = threadIdx.x / (units * sp.groups), rest = threadIdx.x - tr * units * sp.groups;
+    const int t = ((int)blockIdx.x - users.item0[i]) * sp.rows + tr;
+    if (tr >= sp.rows || t >= users.count[i]) return;
     const int64_t row = (int64_t)users.row0[i] + t;
     const int pos = a.fixed ? users.rows[i] : users.rows[i] - users.count[i] + t;
-    const bool rot = rope.rot_dim > 0;
-    if (h >= 2 * kvh) {
-        const int64_t off = (int64_t)(h - 2 * kvh) * a.D;
-        turn_unit<T, VEC>(rope, rot, u, pos, static_cast<const T*>(a.q.p) + row * a.q.ld + off,
-                          static_cast<T*>(a.q_out) + row * a.q_out_ld + off);
-        return;
-    }
-    const bool key = h < kvh;
-    const int kh = key ? h : h - kvh;
-    const int page = pool.tables[(int64_t)users.user[i] * pool.stride + (pos >> pool.page_shift)];
+    const int h0 = rest / units;
+    int page = -1;
+    if (kvh > 0) page = pool.tables[(int64_t)users.user[i] * pool.stride + (pos >> pool.page_shift)];
+    const Unit<VEC> unit(rope, rest % units, pos);
+    if (qh > 0)
+        row_heads<T, VEC, kBatch, true>(unit, h0, sp.groups, qh, a.D, a.D, static_cast<const T*>(a.q.p) + row * a.q.ld,
+                                static_cast<T*>(a.q_out) + row * a.q_out_ld);
     if (page < 0 || page >= pool.n_pages) return;
-    const RowsOf src = key ? a.k : a.v;
-    T* const dst = reinterpret_cast<T*>(pool.data) +
-                   ((((int64_t)page * 2 + (key ? 0 : 1)) * kvh + kh) * pool.page_rows + (pos & (pool.page_rows - 1))) *
-                       a.D;
-    turn_unit<T, VEC>(rope, rot && key, u, pos, static_cast<const T*>(src.p) + row * src.ld + (int64_t)kh * a.D, dst);
+    const int64_t plane = (int64_t)pool.page_rows * a.D;        // one head's rows of the page
+    T* const dst = reinterpret_cast<T*>(pool.data) + (int64_t)page * 2 * kvh * plane +
+                   (int64_t)(pos & (pool.page_rows - 1)) * a.D;
+    row_heads<T, VEC, kBatch, true>(unit, h0, sp.groups, kvh, a.D, plane, static_cast<const T*>(a.k.p) + row * a.k.ld, dst);
+    row_heads<T, VEC, kBatch, false>(unit, h0, sp.groups, kvh, a.D, plane, static_cast<const T*>(a.v.p) + row * a.v.ld,
+                             dst + kvh * plane);
 }
 
 // 16-byte pieces need both halves of the rotated part to be whole pieces.
 template <typename T>
 constexpr int wide() { return 16 / (int)sizeof(T); }
+int vec_of(int dtype, const RopeArgs& rope) {
+    const int v = dtype == UPR_F32 ? wide<float>() : wide<bf16>();
+    return rope.rot_dim % (2 * v) == 0 ? v : 1;
+}
+
+// go(type, VEC, batch) for those values.
+template <typename Go>
+void with_types(int dtype, int vec, int batch, const Go& go) {
+    auto at = [&](auto t, auto v) {
+        if (batch == 1) go(t, v, std::integral_constant<int, 1>{});
+        else go(t, v, std::integral_constant<int, 4>{});
+    };
+    typedef std::integral_constant<int, 1> one;
+    if (dtype == UPR_F32) {
+        if (vec == 1) at(float{}, one{});
+        else at(float{}, std::integral_constant<int, wide<float>()>{});
+    } else {
+        if (vec == 1) at(bf16{}, one{});
+        else at(bf16{}, std::integral_constant<int, wide<bf16>()>{});
+    }
+}
 
 }  // namespace
 
 hipError_t launch_rope(int dtype, const RopeArgs& rope, int heads, int D, RowsOf x, const int32_t* positions,
                        int64_t rows, void* out, int64_t out_ld, hipStream_t s) {
-    auto go = [&](auto t, auto vec) {
+    const int vec = vec_of(dtype, rope), batch = batch_of(rows, heads, D, vec);
+    const int64_t per = split_row(vec, batch, heads, D).rows;
+    with_types(dtype, vec, batch, [&](auto t, auto v, auto b) {
         typedef decltype(t) T;
-        constexpr int VEC = decltype(vec)::value;
-        const int64_t units = rows * heads * (D / (2 * VEC));
-        k_rope<T, VEC><<<(unsigned)((units + 255) / 256), 256, 0, s>>>(rope, heads, D, static_cast<const T*>(x.p),
-                                                                      x.ld, positions, rows, static_cast<T*>(out),
-                                                                      out_ld);
-    };
-    if (dtype == UPR_F32) {
-        if (rope.rot_dim % (2 * wide<float>()) == 0) go(float{}, std::integral_constant<int, wide<float>()>{});
-        else go(float{}, std::integral_constant<int, 1>{});
-    } else {
-        if (rope.rot_dim % (2 * wide<bf16>()) == 0) go(bf16{}, std::integral_constant<int, wide<bf16>()>{});
-        else go(bf16{}, std::integral_constant<int, 1>{});
-    }
+        k_rope<T, decltype(v)::value, decltype(b)::value><<<(unsigned)((rows + per - 1) / per), 256, 0, s>>>(
+            rope, heads, D, static_cast<const T*>(x.p), x.ld, positions, rows, static_cast<T*>(out), out_ld);
+    });
     return hipGetLastError();
 }
 
-static bool append_wide(int dtype, const RopeArgs& rope) {
-    return rope.rot_dim % (2 * (dtype == UPR_F32 ? wide<float>() : wide<bf16>())) == 0;
+static int append_heads(const AppendArgs& a) {
+    return std::max(a.k.p != nullptr ? a.n_kv_heads : 0, a.q.p != nullptr ? a.n_heads : 0);
 }
 
-int64_t append_items(int dtype, const RopeArgs& rope, const AppendArgs& a, int64_t count) {
-    const int vec = append_wide(dtype, rope) ? (dtype == UPR_F32 ? wide<float>() : wide<bf16>()) : 1;
-    const int heads = (a.k.p != nullptr ? 2 * a.n_kv_heads : 0) + (a.q.p != nullptr ? a.n_heads : 0);
-    return (count * heads * (a.D / (2 * vec)) + kAppendUnits - 1) / kAppendUnits;
+int append_batch(int dtype, const RopeArgs& rope, const AppendArgs& a, int64_t rows) {
+    return batch_of(rows, append_heads(a), a.D, vec_of(dtype, rope));
 }
 
-hipError_t launch_append(int dtype, const RopeArgs& rope, const AppendArgs& a, const PagedPool& pool,
+int64_t append_items(int dtype, const RopeArgs& rope, const AppendArgs& a, int batch, int64_t count) {
+    const int64_t per = split_row(vec_of(dtype, rope), batch, append_heads(a), a.D).rows;
+    return (count + per - 1) / per;
+}
+
+hipError_t launch_append(int dtype, const RopeArgs& rope, const AppendArgs& a, int batch, const PagedPool& pool,
                          const PagedUsers& users, hipStream_t s) {
     const unsigned grid = (unsigned)users.item0[users.n];
     if (grid == 0) return hipSuccess;
-    if (dtype == UPR_F32) {
-        if (append_wide(dtype, rope)) k_append<float, wide<float>()><<<grid, 256, 0, s>>>(rope, a, pool, users);
-        else k_append<float, 1><<<grid, 256, 0, s>>>(rope, a, pool, users);
-    } else {
-        if (append_wide(dtype, rope)) k_append<bf16, wide<bf16>()><<<grid, 256, 0, s>>>(rope, a, pool, users);
-        else k_append<bf16, 1><<<grid, 256, 0, s>>>(rope, a, pool, users);
-    }
+    with_types(dtype, vec_of(dtype, rope), batch, [&](auto t, auto v, auto b) {
+        k_append<decltype(t), decltype(v)::value, decltype(b)::value><<<grid, 256, 0, s>>>(rope, a, pool, users);
+    });
     return hipGetLastError();
 }
 

@@ -57,9 +57,11 @@ struct AppendArgs {
     void* q_out;
     int64_t q_out_ld;
 };
-// Work items of `count` rows of one user.
-int64_t append_items(int dtype, const RopeArgs& rope, const AppendArgs& a, int64_t count);
-hipError_t launch_append(int dtype, const RopeArgs& rope, const AppendArgs& a, const PagedPool& pool,
+// Heads per thread for a call of `rows` rows, and the work items of `count`
+// rows of one user.
+int append_batch(int dtype, const RopeArgs& rope, const AppendArgs& a, int64_t rows);
+int64_t append_items(int dtype, const RopeArgs& rope, const AppendArgs& a, int batch, int64_t count);
+hipError_t launch_append(int dtype, const RopeArgs& rope, const AppendArgs& a, int batch, const PagedPool& pool,
                          const PagedUsers& users, hipStream_t s);
 
 // First key that a row at position pos sees, rounded down to a block of keys.

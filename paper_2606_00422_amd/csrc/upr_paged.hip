@@ -173,9 +173,10 @@ static hipError_t each_launch(const upr_segments* seg, const int32_t* rows_host,
 
 hipError_t paged_append(int dtype, const RopeArgs& rope, const AppendArgs& a, const PagedPool& pool,
                         const upr_segments* seg, const int32_t* rows_host, hipStream_t s) {
+    const int batch = append_batch(dtype, rope, a, (int64_t)seg->offsets_host[seg->num_users] - seg->offsets_host[0]);
     return each_launch(
-        seg, rows_host, [&](int32_t c, int32_t) { return append_items(dtype, rope, a, c); },
-        [&](const PagedUsers& u) { return launch_append(dtype, rope, a, pool, u, s); });
+        seg, rows_host, [&](int32_t c, int32_t) { return append_items(dtype, rope, a, batch, c); },
+        [&](const PagedUsers& u) { return launch_append(dtype, rope, a, batch, pool, u, s); });
 }
 
 // ---- the attention's plan

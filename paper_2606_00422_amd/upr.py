@@ -310,6 +310,14 @@ def upr_profile_read() -> dict:
 # Marshalling helpers for torch device tensors (torch supplies memory/streams)
 # ---------------------------------------------------------------------------
 
+def _host_ptr(a: np.ndarray) -> int:
+    """Address of a contiguous array (a fifth of the time of a.ctypes.data)."""
+    try:
+        return ctypes.addressof(ctypes.c_char.from_buffer(a))
+    except (TypeError, ValueError, BufferError):        # read-only or empty
+        return a.ctypes.data
+
+
 def segments(offsets_host: np.ndarray, offsets_dev=None) -> upr_segments:
     """Descriptor over a host int32 offsets array and its device copy (a torch
     int32 tensor).  The caller keeps both alive for the duration of the call."""
@@ -319,7 +327,7 @@ def segments(offsets_host: np.ndarray, offsets_dev=None) -> upr_segments:
     if offsets_dev is not None:
         _check_tensor(offsets_dev, "offsets_dev", "int32")
         dev = offsets_dev.data_ptr()
-    return upr_segments(int(offsets_host.shape[0] - 1), offsets_host.ctypes.data, dev)
+    return upr_segments(int(offsets_host.shape[0] - 1), _host_ptr(offsets_host), dev)
 
 
 def _check_tensor(t, name, dtype=None):
@@ -434,54 +442,75 @@ class KvPool:
 
 
 def current_stream() -> int:
+    """The current device's current stream (the handle alone: making torch's
+    stream object takes 2.8 us)."""
     import torch
-    return int(torch.cuda.current_stream().cuda_stream)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 # ---------------------------------------------------------------------------
 # Paged K/V cache: rotary positions, append, attention
 # ---------------------------------------------------------------------------
 
-def _check_here(t, name):
-    """The library launches on the current device: tensors live there too."""
+def _device() -> int:
+    """The device the library launches on; the tensors of a call live there."""
+    import torch
+    return torch.cuda.current_device()
+
+
+def _check_here(t, name, dev=None):
     import torch
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a GPU tensor")
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    dev = _device() if dev is None else dev
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{dev}")
 
 
-def _paged_dtype(t, name) -> int:
-    code = {"torch.float32": UPR_F32, "torch.bfloat16": UPR_BF16}.get(str(t.dtype))
-    if code is None:
-        raise TypeError(f"{name} must be float32 or bfloat16, got {t.dtype}")
-    return code
+def _check_flat(t, name, dev, dtype):
+    """A contiguous tensor of that torch dtype, here."""
+    _check_here(t, name, dev)
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if not t.is_contiguous():
+        raise TypeError(f"{name} must be contiguous")
 
 
-def _rows3(t, name, like=None, heads=None, dim=None, rows=None):
+def _paged_dtype(dtype, name) -> int:
+    import torch
+    if dtype == torch.bfloat16:
+        return UPR_BF16
+    if dtype == torch.float32:
+        return UPR_F32
+    raise TypeError(f"{name} must be float32 or bfloat16, got {dtype}")
+
+
+def _rows3(t, name, dev, like=None, heads=None, dim=None, rows=0):
     """Pointer and leading dimension of t [rows, heads, head_dim], heads one
     after the other; rows may be strided."""
-    _check_here(t, name)
-    if t.dim() != 3:
+    _check_here(t, name, dev)
+    shape = t.shape
+    if len(shape) != 3:
         raise ValueError(f"{name} must be [rows, heads, head_dim]")
     if like is not None and t.dtype != like:
         raise TypeError(f"{name} must be {like}, got {t.dtype}")
-    if (heads is not None and t.shape[1] != heads) or (dim is not None and t.shape[2] != dim):
-        raise ValueError(f"{name} has {t.shape[1]} heads of {t.shape[2]}, expected {heads} of {dim}")
-    if rows is not None and t.shape[0] < rows:
-        raise ValueError(f"{name} has {t.shape[0]} rows, {rows} needed")
-    if t.shape[0] > 0 and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2])):
+    n, h, d = shape
+    if (heads is not None and h != heads) or (dim is not None and d != dim):
+        raise ValueError(f"{name} has {h} heads of {d}, expected {heads} of {dim}")
+    if n < rows:
+        raise ValueError(f"{name} has {n} rows, {rows} needed")
+    s0, s1, s2 = t.stride()
+    if n > 0 and (s2 != 1 or (h > 1 and s1 != d)):
         raise ValueError(f"{name} must hold each row's heads one after the other")
-    ld = t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1] * t.shape[2])
-    return t.data_ptr(), ld
+    return t.data_ptr(), s0 if n > 1 else max(s0, h * d)
 
 
 def _host_rows(rows_host, users):
-    if not isinstance(rows_host, np.ndarray) or rows_host.dtype != np.int32 or not rows_host.flags["C_CONTIGUOUS"]:
+    if not isinstance(rows_host, np.ndarray) or rows_host.dtype != np.int32 or not rows_host.flags.c_contiguous:
         raise TypeError("rows_host must be a contiguous int32 numpy array")
     if rows_host.shape != (users,):
         raise ValueError(f"rows_host must have one entry per user ({users})")
-    return rows_host.ctypes.data
+    return _host_ptr(rows_host)
 
 
 def _stream_workspace(nbytes: int, stream):
@@ -511,19 +540,21 @@ def rope_apply(x, positions, rope: upr_rope, out=None, stream=None):
     """x [rows, heads, head_dim] rotated, row r at positions[r] (int32), into out
     (a new tensor without one; x itself for in place)."""
     import torch
-    px, ldx = _rows3(x, "x")
+    dev = _device()
+    px, ldx = _rows3(x, "x", dev)
+    rows, heads, dim = x.shape
     if out is None:
         out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    po, ldo = _rows3(out, "out", x.dtype, x.shape[1], x.shape[2])
-    if out.shape[0] != x.shape[0]:
+    po, ldo = (px, ldx) if out is x else _rows3(out, "out", dev, x.dtype, heads, dim)
+    if out.shape[0] != rows:
         raise ValueError("out must have x's shape")
-    _check_here(positions, "positions")
-    _check_tensor(positions, "positions", "int32")
-    if tuple(positions.shape) != (x.shape[0],):
+    _check_flat(positions, "positions", dev, torch.int32)
+    if positions.dim() != 1 or positions.shape[0] != rows:
         raise ValueError("positions must be [rows]")
-    _check(load().upr_rope_apply(ctypes.byref(rope), _paged_dtype(x, "x"), x.shape[1], x.shape[2], px, ldx,
-                                 positions.data_ptr(), x.shape[0], po, ldo,
-                                 current_stream() if stream is None else stream))
+    status = load().upr_rope_apply(rope, _paged_dtype(x.dtype, "x"), heads, dim, px, ldx, positions.data_ptr(), rows,
+                                   po, ldo, current_stream() if stream is None else stream)
+    if status:
+        _check(status)
     return out
 
 
@@ -536,13 +567,15 @@ class PagedCache:
     def __init__(self, data, tables):
         _check_here(data, "data")
         _check_here(tables, "tables")
-        _paged_dtype(data, "data")
+        _paged_dtype(data.dtype, "data")
         if data.dim() not in (5, 6) or data.shape[-4] != 2 or not data.is_contiguous():
             raise ValueError("data must be a contiguous [n_pages, 2, kv_heads, page_rows, head_dim], or "
                              "[n_layers, ...] of it")
         _check_tensor(tables, "tables", "int32")
         if tables.dim() != 2:
             raise ValueError("tables must be [users, pages]")
+        if tables.get_device() != data.get_device():
+            raise ValueError("data and tables must be on one device")
         self.data, self.tables = data, tables
 
     @classmethod
@@ -554,20 +587,25 @@ class PagedCache:
         assert data.numel() * data.element_size() == upr_paged_cache_bytes(c, n_pages, page_rows)
         return cls(data, tables)
 
+    def heads(self):
+        """(kv_heads, head_dim, torch dtype)"""
+        shape = self.data.shape
+        return shape[-3], shape[-1], self.data.dtype
+
     def view(self, users: int, layer=None) -> upr_paged_cache:
         """The C struct, of one layer's plane or (None) of the whole pool."""
-        if self.tables.shape[0] < users:
-            raise ValueError(f"tables has {self.tables.shape[0]} users, {users} needed")
-        data = self.data
-        if layer is not None and data.dim() == 6:
-            data = data[layer]
-        elif layer:
-            raise ValueError("the cache has one plane")
-        return upr_paged_cache(data.data_ptr(), data.shape[-5], data.shape[-2], self.tables.shape[1],
-                               self.tables.data_ptr())
-
-    def shape(self, n_heads: int) -> upr_attn_shape:
-        return upr_attn_shape(_paged_dtype(self.data, "data"), n_heads, self.data.shape[-3], self.data.shape[-1])
+        data, tables = self.data, self.tables
+        _check_here(data, "the cache")
+        held, width = tables.shape
+        if held < users:
+            raise ValueError(f"tables has {held} users, {users} needed")
+        shape = data.shape
+        at = data.data_ptr()
+        if layer is not None and not 0 <= layer < (shape[0] if len(shape) == 6 else 1):
+            raise ValueError(f"the cache has no layer {layer}")
+        if layer:
+            at += layer * data.stride(0) * data.element_size()
+        return upr_paged_cache(at, shape[-5], shape[-2], width, tables.data_ptr())
 
 
 def upr_paged_cache_bytes(cfg: upr_config, n_pages: int, page_rows: int) -> int:
@@ -579,21 +617,23 @@ def paged_append(cache: PagedCache, off_host, rows_host, k, v, rope=None, q=None
     """upr_paged_append on tensors: k and v [rows, kv_heads, head_dim], q and
     q_out [rows, heads, head_dim]; off_host the users' rows, rows_host the rows
     cached when the call ends."""
+    dev = _device()
     seg = segments(off_host)
-    rows = int(off_host[-1])
-    H, D, dt = cache.data.shape[-3], cache.data.shape[-1], cache.data.dtype
-    pk, ldk = _rows3(k, "k", dt, H, D, rows)
-    pv, ldv = _rows3(v, "v", dt, H, D, rows)
+    users, rows = seg.num_users, int(off_host[-1])
+    H, D, dt = cache.heads()
+    pk, ldk = _rows3(k, "k", dev, dt, H, D, rows)
+    pv, ldv = _rows3(v, "v", dev, dt, H, D, rows)
     n_heads, pq, ldq, po, ldo = H, None, 0, None, 0
     if q is not None:
         n_heads = q.shape[1]
-        pq, ldq = _rows3(q, "q", dt, None, D, rows)
+        pq, ldq = _rows3(q, "q", dev, dt, None, D, rows)
     if q_out is not None:
-        po, ldo = _rows3(q_out, "q_out", dt, n_heads, D, rows)
-    _check(load().upr_paged_append(ctypes.byref(cache.shape(n_heads)), ctypes.byref(cache.view(seg.num_users, layer)),
-                                   ctypes.byref(seg), _host_rows(rows_host, seg.num_users),
-                                   None if rope is None else ctypes.byref(rope), pk, ldk, pv, ldv, pq, ldq, po, ldo,
-                                   current_stream() if stream is None else stream))
+        po, ldo = (pq, ldq) if q_out is q else _rows3(q_out, "q_out", dev, dt, n_heads, D, rows)
+    status = load().upr_paged_append(upr_attn_shape(_paged_dtype(dt, "data"), n_heads, H, D), cache.view(users, layer), seg, _host_rows(rows_host, users),
+                                     rope, pk, ldk, pv, ldv, pq, ldq, po, ldo,
+                                     current_stream() if stream is None else stream)
+    if status:
+        _check(status)
 
 
 def _attn_options(scale, softcap, window, slopes, head_dim, k_self=0, v_self=0, self_ld=0) -> upr_attn_options:
@@ -605,11 +645,12 @@ def paged_attention_workspace(cache: PagedCache, off_host, rows_host, n_heads: i
                               own_keys: bool = False, stream=None):
     """Workspace for upr_paged_attention calls of these lengths."""
     seg = segments(off_host)
+    H, D, dt = cache.heads()
     flag = 16 if own_keys else 0            # (not read, only whether it is given)
-    opt = _attn_options(None, 0.0, window, None, cache.data.shape[-1], flag, flag)
+    opt = _attn_options(None, 0.0, window, None, D, flag, flag)
     return _stream_workspace(int(load().upr_paged_attention_workspace_bytes(
-        ctypes.byref(cache.shape(n_heads)), ctypes.byref(cache.view(seg.num_users, 0)), ctypes.byref(seg),
-        _host_rows(rows_host, seg.num_users), ctypes.byref(opt))), stream)
+        upr_attn_shape(_paged_dtype(dt, "data"), n_heads, H, D), cache.view(seg.num_users, 0), seg,
+        _host_rows(rows_host, seg.num_users), opt)), stream)
 
 
 def paged_attention(cache: PagedCache, off_host, rows_host, q, out=None, scale=None, softcap: float = 0.0,
@@ -619,34 +660,35 @@ def paged_attention(cache: PagedCache, off_host, rows_host, q, out=None, scale=N
     [rows, kv_heads, head_dim] for ranking candidates.  scale: 1 /
     sqrt(head_dim) by default."""
     import torch
+    dev = _device()
     seg = segments(off_host)
-    rows = int(off_host[-1])
-    H, D, dt = cache.data.shape[-3], cache.data.shape[-1], cache.data.dtype
-    pq, ldq = _rows3(q, "q", dt, None, D, rows)
+    users, rows = seg.num_users, int(off_host[-1])
+    H, D, dt = cache.heads()
+    pq, ldq = _rows3(q, "q", dev, dt, None, D, rows)
+    n_heads = q.shape[1]
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    po, ldo = _rows3(out, "out", dt, q.shape[1], D, rows)
+    po, ldo = _rows3(out, "out", dev, dt, n_heads, D, rows)
     if slopes is not None:
-        _check_here(slopes, "slopes")
-        _check_tensor(slopes, "slopes", "float32")
-        if tuple(slopes.shape) != (q.shape[1],):
+        _check_flat(slopes, "slopes", dev, torch.float32)
+        if tuple(slopes.shape) != (n_heads,):
             raise ValueError("slopes must be [heads]")
     pks = pvs = lds = 0
     if k_self is not None:
-        pks, lds = _rows3(k_self, "k_self", dt, H, D, rows)
+        pks, lds = _rows3(k_self, "k_self", dev, dt, H, D, rows)
     if v_self is not None:
-        pvs, ldv = _rows3(v_self, "v_self", dt, H, D, rows)
+        pvs, ldv = _rows3(v_self, "v_self", dev, dt, H, D, rows)
         if k_self is not None and ldv != lds:
             raise ValueError("k_self and v_self must have the same row stride")
     opt = _attn_options(scale, softcap, window, slopes, D, pks, pvs, lds)
     if ws is None:
-        ws = paged_attention_workspace(cache, off_host, rows_host, q.shape[1], window, k_self is not None, stream)
-    _check_here(ws, "ws")
-    _check_tensor(ws, "ws", "uint8")
-    _check(load().upr_paged_attention(ctypes.byref(cache.shape(q.shape[1])),
-                                      ctypes.byref(cache.view(seg.num_users, layer)), ctypes.byref(seg),
-                                      _host_rows(rows_host, seg.num_users), ctypes.byref(opt), pq, ldq, po, ldo,
-                                      ws.data_ptr(), ws.numel(), current_stream() if stream is None else stream))
+        ws = paged_attention_workspace(cache, off_host, rows_host, n_heads, window, k_self is not None, stream)
+    _check_flat(ws, "ws", dev, torch.uint8)
+    status = load().upr_paged_attention(upr_attn_shape(_paged_dtype(dt, "data"), n_heads, H, D), cache.view(users, layer), seg, _host_rows(rows_host, users),
+                                        opt, pq, ldq, po, ldo, ws.data_ptr(), ws.numel(),
+                                        current_stream() if stream is None else stream)
+    if status:
+        _check(status)
     return out
 
 
