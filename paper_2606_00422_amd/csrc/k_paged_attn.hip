@@ -68,8 +68,24 @@ __device__ __forceinline__ float quad_sum(float v) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// (NaN if one of them is: no instructions to quiet one first.  Such a row's
+// result is NaN whatever its reference.)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
+}
+
 // 2^x on the transcendental unit (below 2^-126: 0).
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// At most N of the wave's loads (to LDS) still under way; all its LDS reads done.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+    __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | (N >> 4) << 14);
+}
+__device__ __forceinline__ void wait_lds() {
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+}
 
 __device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
 
@@ -187,11 +203,10 @@ template <typename T, int D> __device__ __forceinline__ int key_v(int row) {
     return D == 32 ? ((row >> 2) & 1) << 1 : D == 64 ? ((row >> 1) & 3) << 1 : (row & 7) << 1;
 }
 
-// Keys of a stage: 8 KB or more of each matrix, a whole block per key group.
+// Keys of a stage: a block per key group, or 8 KB and more of each matrix.
 template <typename T, int D, int KW>
 constexpr int stage_keys() {
-    return sizeof(T) == 2 ? (KW == 1 ? (D == 32 ? 128 : 64) : (D == 32 ? 64 : 32) * KW)
-                          : (KW == 1 ? (D == 128 ? 32 : 4096 / D) : D == 128 ? 16 * KW : 4096 / D);
+    return KW > 1 ? (sizeof(T) == 2 ? 32 : 16) * KW : sizeof(T) == 2 ? (D == 32 ? 128 : 64) : D == 128 ? 32 : 4096 / D;
 }
 
 template <typename T, int D, int QG, int RW, int KW, bool EX>
@@ -203,6 +218,7 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void k_paged_attn(AttnArgs a, Page
     constexpr int CR = D * (int)sizeof(T) / 16, RPL = 64 / CR;     // 16-byte chunks per row, rows per load
     constexpr int RPW = TS / NW, NI = RPW / RPL, NP = RPW > 16 ? RPW / 16 : 1;
     constexpr int TR = 16 * QG * RW;
+    static_assert(RW == 1 || KW == 1, "a wave's rows or keys");
     static_assert(KS % SB == 0 && RPW % RPL == 0 && NI >= 1 && NI <= 8 && NP <= 4, "stage");
     __shared__ __attribute__((aligned(16))) T sK0[TS * D];
     __shared__ __attribute__((aligned(16))) T sK1[TS * D];
@@ -237,7 +253,10 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void k_paged_attn(AttnArgs a, Page
     const int wbeg = a.window > 0 ? (own ? n : pfirst) - a.window + 1 : 0;
 
     // ---- K/V stages
-    const int32_t* const table = pool.tables + (int64_t)it.user * pool.stride;
+    // (nothing writes the tables while the kernel runs: scalar loads, which do
+    // not queue behind the stages')
+    typedef const __attribute__((address_space(4))) int32_t* constants;
+    const constants table = (constants)(uintptr_t)(pool.tables + (int64_t)it.user * pool.stride);
     const int64_t block = (int64_t)pool.page_rows * D * (int)sizeof(T);     // one head's rows of a page
     const int rbase = wave * RPW;
     int offK[8], offV[8];
@@ -254,19 +273,20 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void k_paged_attn(AttnArgs a, Page
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
             const int key = k0 + st * TS + rbase + 16 * p;
-            pid[p] = table[(key < n ? key : n - 1) >> pool.page_shift];
+            pid[p] = key < n ? table[key >> pool.page_shift] : -1;
         }
     };
     auto issue_loads = [&](T* dK, T* dV, int st) __attribute__((always_inline)) {
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
             const int key = k0 + st * TS + rbase + 16 * p;
-            const int base = ((key < n ? key : n - 1) >> pool.page_shift) << pool.page_shift;
-            const int page = __builtin_amdgcn_readfirstlane(pid[p]);
-            // rows of the page that hold keys; none in a page outside the pool
-            int valid = n - base < pool.page_rows ? n - base : pool.page_rows;
+            const int base = key & -pool.page_rows;
+            // rows of the page that hold keys; none past the last key or in a
+            // page outside the pool
+            const int page = pid[p];
             const bool in = page >= 0 && page < pool.n_pages;
-            valid = in ? valid : 0;
+            const int rest = n - base < pool.page_rows ? n - base : pool.page_rows;
+            const int valid = in ? rest : 0;
             char* const pk = pool.data + ((int64_t)(in ? page : 0) * 2 * a.n_kv_heads + it.kh) * block;
             const __amdgpu_buffer_rsrc_t rsK =
                 __builtin_amdgcn_make_buffer_rsrc(pk, (short)0, valid * D * (int)sizeof(T), 0x00020000);
@@ -283,11 +303,7 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void k_paged_attn(AttnArgs a, Page
             }
         }
     };
-    if (nst > 0) {
-        fetch_pages(0);
-        issue_loads(sK0, sV0, 0);
-        if (nst > 1) fetch_pages(1);
-    }
+    fetch_pages(0);
 
     // ---- the lane's rows
     typedef std::conditional_t<kBf, b8, f32x4> frag;
@@ -310,11 +326,25 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void k_paged_attn(AttnArgs a, Page
 #pragma unroll
         for (int es = 0; es < ES; ++es)
             qf[qg][es] = *reinterpret_cast<const frag*>(qrow + (kBf ? es * 32 + 8 * g : (4 * es + g) * 4));
+    }
+    // the rows' loads go first: the loop then waits for stages alone
+    __builtin_amdgcn_sched_barrier(0);
+    issue_loads(sK0, sV0, 0);
+    fetch_pages(1);
+    if constexpr (RW == 1) {
+        issue_loads(sK1, sV1, 1);
+        fetch_pages(2);
+    }
+#pragma unroll
+    for (int qg = 0; qg < QG; ++qg) {
         l[qg] = 0.f;
         negm[qg] = -kUnset;
 #pragma unroll
         for (int eb = 0; eb < EB; ++eb) o[qg][eb] = f32x4{0.f, 0.f, 0.f, 0.f};
         if (own && kg == 0 && it.split == 0) {          // starts from the row's own key
+            int r = wrow + qg * 16 + l16;
+            r = r < nrows ? r : nrows - 1;
+            const int64_t row = it.row0 + r / G;
             const T* const krow = static_cast<const T*>(a.k_self.p) + row * a.k_self.ld + (int64_t)it.kh * D;
             const T* const vrow = static_cast<const T*>(a.v_self.p) + row * a.v_self.ld + (int64_t)it.kh * D;
             float s = 0.f;
@@ -338,17 +368,60 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void k_paged_attn(AttnArgs a, Page
         }
     }
 
-    // ---- one block of SB keys: rows kb .. of the stage, keys kabs .. of the user
-    auto sub_block = [&](const T* cK, const T* cV, int kb, int kabs) __attribute__((always_inline)) {
+    // ---- fragments of a block, rows kb .. of the stage
+    constexpr int VW = kBf ? 1 : EB < 4 ? EB : 4;       // fp32: values per read of a V row
+    typedef __attribute__((ext_vector_type(VW))) float vpart;
+    typedef std::conditional_t<kBf, b8, vpart> vfrag;
+    constexpr int NV = kBf ? EB : 4 * (EB / VW);
+    // K: 16-key half t (fp32: the block), step es of the contraction
+    auto read_k = [&](const T* cK, int kb, int t, int es) __attribute__((always_inline)) {
+        const int row = kb + t * 16 + l16;
+        return *reinterpret_cast<const frag*>(
+            &cK[row * D + (((es * 4 + g) ^ key_k<T, D>(row)) << (kBf ? 3 : 2))]);
+    };
+    // V: bf16, V^T of e-block i in the order of the probabilities; fp32, the
+    // part i % (EB / VW) of the lane's columns of row r = i / (EB / VW)
+    auto read_v = [&](const T* cV, int kb, int i) __attribute__((always_inline)) {
+        vfrag vf;
+        if constexpr (kBf) {
+#pragma unroll
+            for (int hh = 0; hh < 2; ++hh) {
+                const int row = kb + 16 * hh + 4 * g + (l16 >> 2);
+                const int ch = 2 * i + ((l16 & 3) >> 1);
+                const T* p = &cV[row * D + ((ch ^ key_v<T, D>(row)) << 3) + ((l16 & 1) << 2)];
+                const b4v v4 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) b4v*)(p));
+#pragma unroll
+                for (int j = 0; j < 4; ++j) vf[4 * hh + j] = v4[j];
+            }
+        } else {
+            vf = *reinterpret_cast<const vfrag*>(cV + (kb + 4 * g + i / (EB / VW)) * D + EB * l16 + i % (EB / VW) * VW);
+        }
+        return vf;
+    };
+    struct Ahead {
+        frag k[NT * ES];
+        vfrag v[NV];
+    };
+
+    // ---- one block of SB keys, keys kabs .. of the user; the fragments from
+    // LDS, or (ahead) read already
+    auto sub_block = [&](const T* cK, const T* cV, int kb, int kabs, const Ahead* ahead) __attribute__((always_inline)) {
+        auto get_k = [&](int t, int es) __attribute__((always_inline)) {
+            if constexpr (RW == 1) return ahead->k[t * ES + es]; else return read_k(cK, kb, t, es);
+        };
+        auto get_v = [&](int i) __attribute__((always_inline)) {
+            if constexpr (RW == 1) return ahead->v[i]; else return read_v(cV, kb, i);
+        };
+        // matrix instructions of a wave go before the other waves' on its SIMD,
+        // whose exponentials then fill the gaps
+        if constexpr (RW > 1) __builtin_amdgcn_s_setprio(1);
         f32x4 s[QG][NT];
         if constexpr (kBf) {
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 b8 kf[ES];
-                const int row = kb + t * 16 + l16;
 #pragma unroll
-                for (int es = 0; es < ES; ++es)
-                    kf[es] = *reinterpret_cast<const b8*>(&cK[row * D + (((es * 4 + g) ^ key_k<T, D>(row)) << 3)]);
+                for (int es = 0; es < ES; ++es) kf[es] = get_k(t, es);
 #pragma unroll
                 for (int qg = 0; qg < QG; ++qg) {
                     s[qg][t] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -362,10 +435,9 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void k_paged_attn(AttnArgs a, Page
             f32x4 so[QG];               // two chains: half the rounding error of one
 #pragma unroll
             for (int qg = 0; qg < QG; ++qg) s[qg][0] = so[qg] = f32x4{0.f, 0.f, 0.f, 0.f};
-            const int row = kb + l16;
 #pragma unroll
             for (int es = 0; es < ES; ++es) {
-                const f32x4 kf = *reinterpret_cast<const f32x4*>(cK + row * D + (((4 * es + g) ^ key_k<T, D>(row)) << 2));
+                const f32x4 kf = get_k(0, es);
 #pragma unroll
                 for (int qg = 0; qg < QG; ++qg)
 #pragma unroll
@@ -378,6 +450,7 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void k_paged_attn(AttnArgs a, Page
 #pragma unroll
             for (int qg = 0; qg < QG; ++qg) s[qg][0] += so[qg];
         }
+        if constexpr (RW > 1) __builtin_amdgcn_s_setprio(0);
         if constexpr (EX) {
 #pragma unroll
             for (int qg = 0; qg < QG; ++qg)
@@ -405,9 +478,8 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void k_paged_attn(AttnArgs a, Page
         bool passed = false;
 #pragma unroll
         for (int qg = 0; qg < QG; ++qg) {
-            float x = fmaxf(fmaxf(s[qg][0][0], s[qg][0][1]), fmaxf(s[qg][0][2], s[qg][0][3]));
-            if constexpr (NT == 2)
-                x = fmaxf(x, fmaxf(fmaxf(s[qg][NT - 1][0], s[qg][NT - 1][1]), fmaxf(s[qg][NT - 1][2], s[qg][NT - 1][3])));
+            float x = max3(max3(s[qg][0][0], s[qg][0][1], s[qg][0][2]), s[qg][0][3], s[qg][NT - 1][0]);
+            if constexpr (NT == 2) x = max3(max3(x, s[qg][1][1], s[qg][1][2]), s[qg][1][3], x);
             top[qg] = x;
             passed |= fmaf(x, c, negm[qg]) > kSlack;
         }
@@ -440,18 +512,10 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void k_paged_attn(AttnArgs a, Page
                     l[qg] = __builtin_amdgcn_fdot2_f32_bf16(pp, ones, l[qg], false);
                 }
             }
+            if constexpr (RW > 1) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int eb = 0; eb < EB; ++eb) {
-                b8 vf;
-#pragma unroll
-                for (int hh = 0; hh < 2; ++hh) {
-                    const int row = kb + 16 * hh + 4 * g + (l16 >> 2);
-                    const int ch = 2 * eb + ((l16 & 3) >> 1);
-                    const T* p = &cV[row * D + ((ch ^ key_v<T, D>(row)) << 3) + ((l16 & 1) << 2)];
-                    const b4v v4 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) b4v*)(p));
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) vf[4 * hh + j] = v4[j];
-                }
+                const b8 vf = get_v(eb);
 #pragma unroll
                 for (int qg = 0; qg < QG; ++qg)
                     o[qg][eb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[qg], o[qg][eb], 0, 0, 0);
@@ -464,52 +528,98 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void k_paged_attn(AttnArgs a, Page
                 for (int r = 0; r < 4; ++r) p[qg][r] = fast_exp2(fmaf(s[qg][0][r], c, negm[qg]));
                 l[qg] += (p[qg][0] + p[qg][1]) + (p[qg][2] + p[qg][3]);
             }
-            constexpr int VW = EB < 4 ? EB : 4;         // values per read of a V row
-            typedef __attribute__((ext_vector_type(VW))) float vrow;
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
+            for (int i = 0; i < NV; ++i) {
+                const vfrag v = get_v(i);
 #pragma unroll
-                for (int j0 = 0; j0 < EB; j0 += VW) {
-                    const vrow v = *reinterpret_cast<const vrow*>(cV + (kb + 4 * g + r) * D + EB * l16 + j0);
+                for (int j = 0; j < VW; ++j)
 #pragma unroll
-                    for (int j = 0; j < VW; ++j)
-#pragma unroll
-                        for (int qg = 0; qg < QG; ++qg)
-                            o[qg][j0 + j] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[j], p[qg][r], o[qg][j0 + j], 0, 0, 0);
-                }
+                    for (int qg = 0; qg < QG; ++qg) {
+                        f32x4& sum = o[qg][i % (EB / VW) * VW + j];
+                        sum = __builtin_amdgcn_mfma_f32_16x16x4f32(v[j], p[qg][i / (EB / VW)], sum, 0, 0, 0);
+                    }
+            }
         }
+        if constexpr (RW > 1) __builtin_amdgcn_s_setprio(0);
         if constexpr (kBf) mfma_settled<8>(); else mfma_settled<16>();
     };
 
-    auto stage = [&](const T* cK, const T* cV, T* nK, T* nV, int st) __attribute__((always_inline)) {
-        if (st + 1 < nst) {
-            issue_loads(nK, nV, st + 1);
-            if (st + 2 < nst) fetch_pages(st + 2);
-        }
-        if (active) {
+    if constexpr (RW == 1) {
+        // A wave loads the very rows that it reads: no barriers.  Two stages are
+        // under way to LDS and one from there to registers while a block is
+        // computed.  (Stages past the last are loads of nothing: without
+        // branches around them the compiler knows that the rows have landed.)
+        static_assert(KS == SB, "one block per stage");
+        auto read_ahead = [&](const T* cK, const T* cV, Ahead& f) __attribute__((always_inline)) {
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int i = 0; i < KS / SB; ++i) {
-                const int kb = kg * KS + i * SB, kabs = k0 + st * TS + kb;
-                if (kabs < k1 && kabs < wend && kabs + SB > wbeg) sub_block(cK, cV, kb, kabs);
-            }
+            for (int i = 0; i < NT * ES; ++i) f.k[i] = read_k(cK, kg * KS, i / ES, i % ES);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) f.v[i] = read_v(cV, kg * KS, i);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        // computes stage st (its fragments in cur), reads stage st + 1 from LDS
+        // and loads stage st + 2 where st was
+        auto stage = [&](T* cK, T* cV, const T* nK, const T* nV, const Ahead& cur, Ahead& next, int st)
+            __attribute__((always_inline)) {
+            wait_lds();
+            issue_loads(cK, cV, st + 2);
+            fetch_pages(st + 3);
+            wait_loads<2 * NI>();
+            read_ahead(nK, nV, next);
+            const int kabs = k0 + st * TS + kg * KS;
+            if (kabs < k1 && kabs < wend && kabs + SB > wbeg) sub_block(cK, cV, 0, kabs, &cur);
+        };
+        wait_loads<4 * NI>();           // the rows
+        wait_loads<2 * NI>();           // the first stage
+        Ahead f0, f1;
+        read_ahead(sK0, sV0, f0);
+        int st = 0;
+        for (; st + 2 <= nst; st += 2) {
+            stage(sK0, sV0, sK1, sV1, f0, f1, st);
+            stage(sK1, sV1, sK0, sV0, f1, f0, st + 1);
         }
-        __builtin_amdgcn_s_waitcnt(0x0F70);     // vmcnt(0): next stage landed
+        if (st < nst) stage(sK0, sV0, sK1, sV1, f0, f1, st);
+        wait_lds();
+        wait_loads<0>();
+        __syncthreads();        // (the merge writes over other waves' rows)
+    } else {
+        auto stage = [&](const T* cK, const T* cV, T* nK, T* nV, int st) __attribute__((always_inline)) {
+            if (st + 1 < nst) {
+                issue_loads(nK, nV, st + 1);
+                fetch_pages(st + 2);
+            }
+            if (active) {
+#pragma unroll
+                for (int i = 0; i < KS / SB; ++i) {
+                    const int kabs = k0 + st * TS + i * SB;
+                    if (kabs < k1 && kabs < wend && kabs + SB > wbeg) sub_block(cK, cV, i * SB, kabs, nullptr);
+                }
+            }
+            wait_loads<0>();                    // next stage landed
+            __syncthreads();
+        };
+        wait_loads<0>();
         __syncthreads();
-    };
-    if (nst > 0) __builtin_amdgcn_s_waitcnt(0x0F70);
-    __syncthreads();
-    int st = 0;
-    for (; st + 2 <= nst; st += 2) {
-        stage(sK0, sV0, sK1, sV1, st);
-        stage(sK1, sV1, sK0, sV0, st + 1);
+        int st = 0;
+        for (; st + 2 <= nst; st += 2) {
+            stage(sK0, sV0, sK1, sV1, st);
+            stage(sK1, sV1, sK0, sV0, st + 1);
+        }
+        if (st < nst) stage(sK0, sV0, sK1, sV1, st);
     }
-    if (st < nst) stage(sK0, sV0, sK1, sV1, st);
 
     // ---- key groups meet in LDS (all reads of the stages ended at the last barrier)
     if constexpr (KW > 1) {
-        constexpr int kWords = QG * (EB * 4 + 2);
-        static_assert(RW * kWords * 64 * 4 <= TS * D * (int)sizeof(T) && KW <= 4, "merge space");
-        float* const x = reinterpret_cast<float*>(kg == 1 ? sK0 : kg == 2 ? sK1 : sV0) + rw * kWords * 64 + lane;
+        // one slot per wave but the first group's, as many per array as fit
+        constexpr int kWords = QG * (EB * 4 + 2), kSlots = TS * D * (int)sizeof(T) / (kWords * 256);
+        static_assert(RW == 1 && kSlots >= 1 && 4 * kSlots >= KW - 1, "merge space");
+        auto slot = [&](int w) __attribute__((always_inline)) {
+            const int i = (w - 1) / kSlots;
+            return reinterpret_cast<float*>(i == 0 ? sK0 : i == 1 ? sK1 : i == 2 ? sV0 : sV1) +
+                   (w - 1) % kSlots * kWords * 64 + lane;
+        };
+        float* const x = slot(kg > 0 ? kg : 1);
         if (kg > 0) {
 #pragma unroll
             for (int qg = 0; qg < QG; ++qg) {
@@ -525,7 +635,7 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void k_paged_attn(AttnArgs a, Page
         if (kg > 0) return;
 #pragma unroll
         for (int w = 1; w < KW; ++w) {
-            const float* const y = reinterpret_cast<const float*>(w == 1 ? sK0 : w == 2 ? sK1 : sV0) + rw * kWords * 64 + lane;
+            const float* const y = slot(w);
 #pragma unroll
             for (int qg = 0; qg < QG; ++qg) {
                 const float nw = y[(qg * (EB * 4 + 2) + EB * 4) * 64];
@@ -595,16 +705,14 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void k_paged_attn(AttnArgs a, Page
                             b4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
                 }
             } else {
-                constexpr int VW = EB < 4 ? EB : 4;
-                typedef __attribute__((ext_vector_type(VW))) float vrow;
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
                     for (int j0 = 0; j0 < EB; j0 += VW) {
-                        vrow v;
+                        vpart v;
 #pragma unroll
                         for (int j = 0; j < VW; ++j) v[j] = o[qg][j0 + j][i];
-                        *reinterpret_cast<vrow*>(static_cast<float*>(a.out) + at + EB * (4 * g + i) + j0) = v;
+                        *reinterpret_cast<vpart*>(static_cast<float*>(a.out) + at + EB * (4 * g + i) + j0) = v;
                     }
             }
         }
@@ -630,32 +738,51 @@ __global__ __launch_bounds__(256) void k_paged_attn_join(AttnArgs a, PagedPool p
     const int G = a.n_heads / a.n_kv_heads, nrows = it.count * G, tile0 = it.tile * TR;
     const int here = nrows - tile0 < TR ? nrows - tile0 : TR;
     constexpr int kE = D > 64 ? D / 64 : 1;
+    // lane j of part s: values E j .. E j + E - 1, of every PP-th part
+    constexpr int E = D / 32, PP = 2;
+    typedef __attribute__((ext_vector_type(E))) float part;
+    const int e0 = (lane & 31) * E, half = lane >> 5;
     for (int i = wave; i < here; i += 4) {
-        auto rec = [&](int s) { return ((int64_t)blockIdx.x + (int64_t)s * a.n_kv_heads) * TR + i; };
-        float nm = -kUnset;
-        for (int s = lane; s < it.splits; s += 64) nm = fminf(nm, a.part_ml[2 * rec(s)]);
-        nm = -wave_max(-nm);
-        float l = 0.f, acc[kE];
-        for (int j = 0; j < kE; ++j) acc[j] = 0.f;
-        for (int s = 0; s < it.splits; ++s) {
-            const int64_t rs = rec(s);
-            const float w = fast_exp2(nm - a.part_ml[2 * rs]);
-            l = fmaf(w, a.part_ml[2 * rs + 1], l);
+        const int64_t rec0 = (int64_t)blockIdx.x * TR + i, step = (int64_t)a.n_kv_heads * TR;
+        float nm = -kUnset, l = 0.f, acc[E];
 #pragma unroll
-            for (int j = 0; j < kE; ++j) acc[j] = fmaf(w, a.part_o[rs * D + j * 64 + lane % D], acc[j]);
+        for (int j = 0; j < E; ++j) acc[j] = 0.f;
+        for (int s0 = 0; s0 < it.splits; s0 += 64) {
+            // 64 parts' references and sums, one per lane
+            const int left = it.splits - s0 < 64 ? it.splits - s0 : 64;
+            const int64_t rs = rec0 + (int64_t)(s0 + (lane < left ? lane : 0)) * step;
+            const float ns = lane < left ? a.part_ml[2 * rs] : -kUnset;
+            const float ls = lane < left ? a.part_ml[2 * rs + 1] : 0.f;
+            const float nn = fminf(nm, -wave_max(-ns));
+            const float alpha = fast_exp2(nn - nm), w = fast_exp2(nn - ns);
+            nm = nn;
+            l = l * alpha + wave_sum(w * ls);
+#pragma unroll
+            for (int j = 0; j < E; ++j) acc[j] *= alpha;
+            // their outputs, PP at a time, eight loads under way
+#pragma unroll 8
+            for (int s = 0; s < left; s += PP) {
+                const int mine = s + half < left ? s + half : s;
+                const part v = *reinterpret_cast<const part*>(a.part_o + (rec0 + (int64_t)(s0 + mine) * step) * D + e0);
+                const float ws = s + half < left ? __shfl(w, mine, 64) : 0.f;
+#pragma unroll
+                for (int j = 0; j < E; ++j) acc[j] = fmaf(ws, v[j], acc[j]);
+            }
         }
+#pragma unroll
+        for (int j = 0; j < E; ++j) acc[j] += __shfl_xor(acc[j], 32, 64);
         const float inv = 1.f / l;
         bool bad = !finite(inv) || !(inv > 0.f);
         const int r = tile0 + i, t = r / G, h = it.kh * G + (r - t * G);
-        const int64_t row = it.row0 + t, at = row * a.out_ld + (int64_t)h * D;
+        const int64_t row = it.row0 + t, at = row * a.out_ld + (int64_t)h * D + e0;
 #pragma unroll
-        for (int j = 0; j < kE; ++j) {
+        for (int j = 0; j < E; ++j) {
             const float v = keep_f32(acc[j] * inv);
             bad |= !finite(v);
-            if (lane >= D) continue;
-            if (a.out_kind == ATTN_OUT_F16) static_cast<f16*>(a.out)[at + j * 64 + lane] = (f16)v;
-            else if (a.out_kind == ATTN_OUT_F32) static_cast<float*>(a.out)[at + j * 64 + lane] = v;
-            else static_cast<T*>(a.out)[at + j * 64 + lane] = (T)v;
+            if (half) continue;
+            if (a.out_kind == ATTN_OUT_F16) static_cast<f16*>(a.out)[at + j] = (f16)v;
+            else if (a.out_kind == ATTN_OUT_F32) static_cast<float*>(a.out)[at + j] = v;
+            else static_cast<T*>(a.out)[at + j] = (T)v;
         }
         if (__any(bad))
             attn_row<T, D>(a, pool, it.user, it.rows, row, a.k_self.p != nullptr ? it.rows : it.rows - it.count + t, h);
@@ -678,6 +805,8 @@ hipError_t launch_tiles(const AttnArgs& a, const PagedPool& pool, const PagedUse
 template <typename T, int D>
 hipError_t launch_dim(const AttnArgs& a, const PagedPool& pool, const PagedUsers& users, bool join, hipStream_t s) {
     constexpr bool bf = sizeof(T) == 2;
+    if constexpr (D < 128)
+        if (a.tile == 16 && a.waves == 8) return launch_tiles<T, D, 1, 1, 8>(a, pool, users, join, s);
     if (a.tile == 16) return launch_tiles<T, D, 1, 1, 4>(a, pool, users, join, s);
     if constexpr (bf) {
         if (a.tile == 32) return launch_tiles<T, D, 2, 1, 4>(a, pool, users, join, s);

@@ -2,6 +2,7 @@
 // and the launches of upr_rope_*, upr_paged_append and upr_paged_attention.
 #include <algorithm>
 #include <cmath>
+#include <cstdlib>
 
 #include "upr_paged_host.h"
 #include "upr_profile.h"
@@ -180,6 +181,7 @@ hipError_t paged_append(int dtype, const RopeArgs& rope, const AppendArgs& a, co
 }
 
 // ---- the attention's plan
+static int env_int(const char* n, int d) { const char* e = getenv(n); return e ? atoi(e) : d; }
 
 static int64_t attn_user_items(const AttnArgs& a, int32_t count, int32_t rows) {
     const int64_t tiles = ((int64_t)count * (a.n_heads / a.n_kv_heads) + a.tile - 1) / a.tile;
@@ -210,15 +212,26 @@ static size_t plan_attn(int dtype, AttnArgs* a, const upr_segments* seg, const i
         a->tile = 16;
     } else if (dtype == UPR_F32) {
         a->tile = 64;
+        if (items_of(64, &keys) < env_int("UPR_T64", 512)) a->tile = 16;
     } else {
         a->tile = 128;
-        if (items_of(128, &keys) < 512) a->tile = 32;
+        if (items_of(128, &keys) < env_int("UPR_T128", 512)) a->tile = 32;
     }
     const int64_t items = items_of(a->tile, &keys);
-    if (items > 0 && items < 1024) {
+    a->waves = 4;
+    int64_t longest = 0;
+    for (int u = 0; u < seg->num_users; ++u)
+        if (o[u + 1] > o[u])
+            longest = std::max<int64_t>(longest, rows_host[u] - attn_first_key(a->k_self.p ? rows_host[u] : rows_host[u] - (o[u + 1] - o[u]), a->window));
+    if (a->tile == 16 && a->D < 128 && longest <= env_int("UPR_ALONE", 2048)) {
+        a->waves = 8;
+        return 0;
+    }
+    if (a->tile == 16 && a->D < 128) a->waves = env_int("UPR_WAVES", 4);
+    if (items > 0 && items < env_int("UPR_MAXITEMS", 1024)) {
         // parts of equal length, whole stages, none below 512 keys
-        const double per = keys / 1024;
-        const int64_t chunk = std::max<int64_t>(512, ((int64_t)per + 255) / 256 * 256);
+        const double per = keys / env_int("UPR_TARGET", 1024);
+        const int64_t chunk = std::max<int64_t>(env_int("UPR_MINCHUNK", 512), ((int64_t)per + 255) / 256 * 256);
         a->chunk = (int32_t)std::min<int64_t>(chunk, 1 << 30);
     }
     if (a->chunk == 0) return 0;
