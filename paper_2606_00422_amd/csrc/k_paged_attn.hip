@@ -87,17 +87,19 @@ __device__ __forceinline__ void wait_lds() {
     __builtin_amdgcn_s_waitcnt(0xC07F);
 }
 
+__device__ __forceinline__ float first_of(float x) { return x; }
+__device__ __forceinline__ float first_of(f32x4 x) { return x[0]; }
+
 __device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
 
-// Score in log2 units.  tanh x = 1 - 2 / (2^(2 x log2 e) + 1), off by about
-// 2^-23: the cap is far above any difference of scores that matters.
+// The capped score in log2 units.  tanh x = 1 - 2 / (2^(2 x log2 e) + 1), off by
+// about 2^-23: the cap is far above any difference of scores that matters.
+__device__ __forceinline__ float capped(const AttnArgs& a, float dot) {
+    return a.cap2 * fmaf(-2.f, __builtin_amdgcn_rcpf(fast_exp2(dot * a.ct2) + 1.f), 1.f);
+}
+// Score in log2 units.
 __device__ __forceinline__ float score2(const AttnArgs& a, float dot, float slope2, int away) {
-    float z = dot * a.c;
-    if (a.cap2 > 0.f) {
-        const float t = fast_exp2(dot * a.ct2);
-        z = a.cap2 * fmaf(-2.f, __builtin_amdgcn_rcpf(t + 1.f), 1.f);
-    }
-    return fmaf(slope2, (float)away, z);
+    return fmaf(slope2, (float)away, a.cap2 > 0.f ? capped(a, dot) : dot * a.c);
 }
 
 // Where an item stands.
@@ -125,6 +127,23 @@ __device__ __forceinline__ Item find_item(const AttnArgs& a, const PagedUsers& u
     if (a.k_self.p == nullptr) it.tile = (it.count * (a.n_heads / a.n_kv_heads) + TR - 1) / TR - 1 - it.tile;
     return it;
 }
+
+// Rows of a tile as (token, head of the group): one division for the tile, the
+// rest by multiplication (x below 2048 and G at most 1024: exact).
+struct Rows {
+    int G, t0, h0;
+    uint32_t magic;             // 2^32 / G, rounded up
+
+    __device__ __forceinline__ Rows(int group, int tile0) : G(group), t0(tile0 / group) {
+        h0 = tile0 - t0 * G;
+        magic = 0xffffffffu / (uint32_t)G + 1;
+    }
+    // row i of the tile: its token, and its head in the group
+    __device__ __forceinline__ int token(int i) const {
+        return t0 + (G == 1 ? i : (int)__umulhi((uint32_t)(h0 + i), magic));
+    }
+    __device__ __forceinline__ int head(int i, int t) const { return h0 + i - (t - t0) * G; }
+};
 
 // One row by one wave, from its visible keys alone (speed is of no concern).
 template <typename T, int D>
@@ -210,7 +229,7 @@ constexpr int stage_keys() {
 }
 
 template <typename T, int D, int QG, int RW, int KW, bool EX>
-__global__ __launch_bounds__(64 * RW * KW, 2) void k_paged_attn(AttnArgs a, PagedPool pool, PagedUsers users) {
+__global__ __launch_bounds__(64 * RW * KW, RW > 1 && D < 128 ? (EX ? 3 : 4) : 2) void k_paged_attn(AttnArgs a, PagedPool pool, PagedUsers users) {
     constexpr bool kBf = sizeof(T) == 2;
     constexpr int NW = RW * KW, SB = kBf ? 32 : 16, NT = SB / 16;
     constexpr int TS = stage_keys<T, D, KW>(), KS = TS / KW;
@@ -237,8 +256,9 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void k_paged_attn(AttnArgs a, Page
     const int tile0 = it.tile * TR;
     const int tlast = (tile0 + TR < nrows ? tile0 + TR : nrows) - 1;
     // keys of the tile, then of this part of them
-    const int end = own ? n : pos0 + tlast / G + 1;
-    const int first = attn_first_key(own ? n : pos0 + tile0 / G, a.window);
+    const Rows rows(G, tile0);
+    const int end = own ? n : pos0 + rows.token(tlast - tile0) + 1;
+    const int first = attn_first_key(own ? n : pos0 + rows.t0, a.window);
     const int k0 = a.chunk > 0 ? first + it.split * a.chunk : first;
     const int k1 = a.chunk > 0 && k0 + a.chunk < end ? k0 + a.chunk : end;
     const int nst = k1 > k0 ? (k1 - k0 + TS - 1) / TS : 0;
@@ -246,7 +266,8 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void k_paged_attn(AttnArgs a, Page
     const int wrow = tile0 + rw * 16 * QG;
     const bool active = wrow < nrows;
     const int wlast = wrow + 16 * QG < nrows ? wrow + 16 * QG - 1 : nrows - 1;
-    const int pfirst = own ? n - 1 : pos0 + wrow / G, plast = own ? n - 1 : pos0 + wlast / G;
+    const int pfirst = own ? n - 1 : pos0 + rows.token(wrow - tile0);
+    const int plast = own ? n - 1 : pos0 + rows.token(wlast - tile0);
     const int wend = plast + 1;                         // keys from here on: none for the wave
     // keys below this one are outside the last row's window, from wbeg on inside the first row's
     const int wlow = a.window > 0 ? (own ? n : plast) - a.window + 1 : 0;
@@ -309,13 +330,19 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void k_paged_attn(AttnArgs a, Page
     typedef std::conditional_t<kBf, b8, f32x4> frag;
     frag qf[QG][ES];
     f32x4 o[QG][EB];            // bf16: e = 16 eb + 4g + r; fp32: e = EB (4g + r) + eb
-    float l[QG], negm[QG], slope2[QG];
+    // row sums: the product of the probabilities with ones (the sum of all keys
+    // so far, in all four registers), or where those registers are short (128 for
+    // four waves per SIMD), and in fp32, of the lane's keys
+    constexpr bool kOnes = kBf && (RW == 1 || D == 128);
+    typedef std::conditional_t<kOnes, f32x4, float> lsum;
+    lsum l[QG];
+    float negm[QG], slope2[QG];
     int rpos[QG], low[QG], seen[QG];
 #pragma unroll
     for (int qg = 0; qg < QG; ++qg) {
         int r = wrow + qg * 16 + l16;
         r = r < nrows ? r : nrows - 1;                  // (a ragged tail repeats the last row)
-        const int t = r / G, h = it.kh * G + (r - t * G);
+        const int t = rows.token(r - tile0), h = it.kh * G + rows.head(r - tile0, t);
         const int64_t row = it.row0 + t;
         rpos[qg] = pos0 + (own ? 0 : t);
         low[qg] = a.window > 0 && rpos[qg] >= a.window ? rpos[qg] - a.window + 1 : 0;
@@ -337,14 +364,14 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void k_paged_attn(AttnArgs a, Page
     }
 #pragma unroll
     for (int qg = 0; qg < QG; ++qg) {
-        l[qg] = 0.f;
+        l[qg] = lsum{0.f};
         negm[qg] = -kUnset;
 #pragma unroll
         for (int eb = 0; eb < EB; ++eb) o[qg][eb] = f32x4{0.f, 0.f, 0.f, 0.f};
         if (own && kg == 0 && it.split == 0) {          // starts from the row's own key
             int r = wrow + qg * 16 + l16;
             r = r < nrows ? r : nrows - 1;
-            const int64_t row = it.row0 + r / G;
+            const int64_t row = it.row0 + rows.token(r - tile0);
             const T* const krow = static_cast<const T*>(a.k_self.p) + row * a.k_self.ld + (int64_t)it.kh * D;
             const T* const vrow = static_cast<const T*>(a.v_self.p) + row * a.v_self.ld + (int64_t)it.kh * D;
             float s = 0.f;
@@ -357,9 +384,9 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void k_paged_attn(AttnArgs a, Page
             const float z = score2(a, quad_sum(s), 0.f, 0);
             if (z > kUnset) {                           // (else: attn_row, as for any row out of range)
                 negm[qg] = -z;
-                l[qg] = g == 0 ? 1.f : 0.f;
+                if constexpr (kOnes) l[qg] = f32x4{1.f, 1.f, 1.f, 1.f}; else l[qg] = g == 0 ? 1.f : 0.f;
             } else {
-                l[qg] = NAN;
+                if constexpr (kOnes) l[qg] = f32x4{NAN, NAN, NAN, NAN}; else l[qg] = NAN;
             }
 #pragma unroll
             for (int eb = 0; eb < EB; ++eb)
@@ -398,20 +425,24 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void k_paged_attn(AttnArgs a, Page
         }
         return vf;
     };
-    struct Ahead {
+    struct Frags {
         frag k[NT * ES];
         vfrag v[NV];
     };
+    auto read_ks = [&](const T* cK, int kb, Frags& f) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < NT * ES; ++i) f.k[i] = read_k(cK, kb, i / ES, i % ES);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto read_vs = [&](const T* cV, int kb, Frags& f) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) f.v[i] = read_v(cV, kb, i);
+        __builtin_amdgcn_sched_barrier(0);
+    };
 
-    // ---- one block of SB keys, keys kabs .. of the user; the fragments from
-    // LDS, or (ahead) read already
-    auto sub_block = [&](const T* cK, const T* cV, int kb, int kabs, const Ahead* ahead) __attribute__((always_inline)) {
-        auto get_k = [&](int t, int es) __attribute__((always_inline)) {
-            if constexpr (RW == 1) return ahead->k[t * ES + es]; else return read_k(cK, kb, t, es);
-        };
-        auto get_v = [&](int i) __attribute__((always_inline)) {
-            if constexpr (RW == 1) return ahead->v[i]; else return read_v(cV, kb, i);
-        };
+    // ---- one block of SB keys, keys kabs .. of the user, from its fragments;
+    // scored(): called when those of K are used up
+    auto sub_block = [&](const Frags& f, int kabs, auto scored) __attribute__((always_inline)) {
         // matrix instructions of a wave go before the other waves' on its SIMD,
         // whose exponentials then fill the gaps
         if constexpr (RW > 1) __builtin_amdgcn_s_setprio(1);
@@ -421,7 +452,7 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void k_paged_attn(AttnArgs a, Page
             for (int t = 0; t < NT; ++t) {
                 b8 kf[ES];
 #pragma unroll
-                for (int es = 0; es < ES; ++es) kf[es] = get_k(t, es);
+                for (int es = 0; es < ES; ++es) kf[es] = f.k[t * ES + es];
 #pragma unroll
                 for (int qg = 0; qg < QG; ++qg) {
                     s[qg][t] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -437,7 +468,7 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void k_paged_attn(AttnArgs a, Page
             for (int qg = 0; qg < QG; ++qg) s[qg][0] = so[qg] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int es = 0; es < ES; ++es) {
-                const f32x4 kf = get_k(0, es);
+                const f32x4 kf = f.k[es];
 #pragma unroll
                 for (int qg = 0; qg < QG; ++qg)
 #pragma unroll
@@ -451,27 +482,45 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void k_paged_attn(AttnArgs a, Page
             for (int qg = 0; qg < QG; ++qg) s[qg][0] += so[qg];
         }
         if constexpr (RW > 1) __builtin_amdgcn_s_setprio(0);
+        scored();
         if constexpr (EX) {
+            if (a.cap2 > 0.f) {
 #pragma unroll
-            for (int qg = 0; qg < QG; ++qg)
+                for (int qg = 0; qg < QG; ++qg)
 #pragma unroll
-                for (int t = 0; t < NT; ++t)
+                    for (int t = 0; t < NT; ++t)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        s[qg][t][r] = score2(a, s[qg][t][r], slope2[qg], kabs + t * 16 + 4 * g + r - rpos[qg]);
+                        for (int r = 0; r < 4; ++r) s[qg][t][r] = capped(a, s[qg][t][r]);
+            } else {
+#pragma unroll
+                for (int qg = 0; qg < QG; ++qg)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) s[qg][t][r] *= a.c;
+            }
+            if (a.slopes != nullptr) {
+#pragma unroll
+                for (int qg = 0; qg < QG; ++qg) {
+                    const float away = (float)(kabs + 4 * g - rpos[qg]);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) s[qg][t][r] = fmaf(slope2[qg], away + (float)(16 * t + r), s[qg][t][r]);
+                }
+            }
         }
         const float c = EX ? 1.f : a.c;
         // keys after a row, past the cache, or behind its window
         if (__builtin_expect(kabs + SB > pfirst + 1 || kabs + SB > k1 || kabs < wlow, 0)) {
 #pragma unroll
-            for (int qg = 0; qg < QG; ++qg)
+            for (int qg = 0; qg < QG; ++qg) {
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        // keys seen: low .. low + seen - 1
+                    for (int r = 0; r < 4; ++r)         // keys seen: low .. low + seen - 1
                         if ((unsigned)(kabs + t * 16 + 4 * g + r - low[qg]) >= (unsigned)seen[qg]) s[qg][t][r] = -INFINITY;
-                    }
+            }
         }
         // references that are passed by too much
         float top[QG];
@@ -505,17 +554,24 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void k_paged_attn(AttnArgs a, Page
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) pf[qg][t * 4 + r] = (__bf16)fast_exp2(fmaf(s[qg][t][r], c, negm[qg]));
-                const b2 ones = {(__bf16)1.0f, (__bf16)1.0f};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const b2 pp = {pf[qg][2 * j], pf[qg][2 * j + 1]};
-                    l[qg] = __builtin_amdgcn_fdot2_f32_bf16(pp, ones, l[qg], false);
-                }
             }
             if constexpr (RW > 1) __builtin_amdgcn_s_setprio(1);
+            const __bf16 u = (__bf16)1.0f;
+            if constexpr (kOnes) {
+                const b8 ones = {u, u, u, u, u, u, u, u};
+#pragma unroll
+                for (int qg = 0; qg < QG; ++qg)
+                    l[qg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[qg], l[qg], 0, 0, 0);
+            } else {
+#pragma unroll
+                for (int qg = 0; qg < QG; ++qg)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        l[qg] = __builtin_amdgcn_fdot2_f32_bf16(b2{pf[qg][2 * j], pf[qg][2 * j + 1]}, b2{u, u}, l[qg], false);
+            }
 #pragma unroll
             for (int eb = 0; eb < EB; ++eb) {
-                const b8 vf = get_v(eb);
+                const b8 vf = f.v[eb];
 #pragma unroll
                 for (int qg = 0; qg < QG; ++qg)
                     o[qg][eb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[qg], o[qg][eb], 0, 0, 0);
@@ -530,7 +586,7 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void k_paged_attn(AttnArgs a, Page
             }
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const vfrag v = get_v(i);
+                const vfrag v = f.v[i];
 #pragma unroll
                 for (int j = 0; j < VW; ++j)
 #pragma unroll
@@ -550,30 +606,26 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void k_paged_attn(AttnArgs a, Page
         // computed.  (Stages past the last are loads of nothing: without
         // branches around them the compiler knows that the rows have landed.)
         static_assert(KS == SB, "one block per stage");
-        auto read_ahead = [&](const T* cK, const T* cV, Ahead& f) __attribute__((always_inline)) {
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int i = 0; i < NT * ES; ++i) f.k[i] = read_k(cK, kg * KS, i / ES, i % ES);
-#pragma unroll
-            for (int i = 0; i < NV; ++i) f.v[i] = read_v(cV, kg * KS, i);
-            __builtin_amdgcn_sched_barrier(0);
-        };
         // computes stage st (its fragments in cur), reads stage st + 1 from LDS
         // and loads stage st + 2 where st was
-        auto stage = [&](T* cK, T* cV, const T* nK, const T* nV, const Ahead& cur, Ahead& next, int st)
+        auto stage = [&](T* cK, T* cV, const T* nK, const T* nV, const Frags& cur, Frags& next, int st)
             __attribute__((always_inline)) {
             wait_lds();
             issue_loads(cK, cV, st + 2);
             fetch_pages(st + 3);
             wait_loads<2 * NI>();
-            read_ahead(nK, nV, next);
+            __builtin_amdgcn_sched_barrier(0);
+            read_ks(nK, kg * KS, next);
+            read_vs(nV, kg * KS, next);
             const int kabs = k0 + st * TS + kg * KS;
-            if (kabs < k1 && kabs < wend && kabs + SB > wbeg) sub_block(cK, cV, 0, kabs, &cur);
+            if (kabs < k1 && kabs < wend && kabs + SB > wbeg) sub_block(cur, kabs, [] {});
         };
         wait_loads<4 * NI>();           // the rows
         wait_loads<2 * NI>();           // the first stage
-        Ahead f0, f1;
-        read_ahead(sK0, sV0, f0);
+        Frags f0, f1;
+        __builtin_amdgcn_sched_barrier(0);
+        read_ks(sK0, kg * KS, f0);
+        read_vs(sV0, kg * KS, f0);
         int st = 0;
         for (; st + 2 <= nst; st += 2) {
             stage(sK0, sV0, sK1, sV1, f0, f1, st);
@@ -590,10 +642,29 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void k_paged_attn(AttnArgs a, Page
                 fetch_pages(st + 2);
             }
             if (active) {
+                // a block's V is read before its scores, the next block's K
+                // while its probabilities are computed
+                constexpr bool kDeep = D == 128;
+                Frags f;
+                bool have = false;
 #pragma unroll
                 for (int i = 0; i < KS / SB; ++i) {
                     const int kabs = k0 + st * TS + i * SB;
-                    if (kabs < k1 && kabs < wend && kabs + SB > wbeg) sub_block(cK, cV, i * SB, kabs, nullptr);
+                    if (!(kabs < k1 && kabs < wend && kabs + SB > wbeg)) {
+                        have = false;
+                        continue;
+                    }
+                    if constexpr (kDeep) {
+                        if (!have) read_ks(cK, i * SB, f);
+                        read_vs(cV, i * SB, f);
+                        sub_block(f, kabs, [&] {
+                            if (i + 1 < KS / SB) read_ks(cK, i * SB + SB, f);
+                        });
+                        have = true;
+                    } else {
+                        read_ks(cK, i * SB, f);
+                        sub_block(f, kabs, [&] { read_vs(cV, i * SB, f); });
+                    }
                 }
             }
             wait_loads<0>();                    // next stage landed
@@ -628,7 +699,7 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void k_paged_attn(AttnArgs a, Page
 #pragma unroll
                     for (int r = 0; r < 4; ++r) x[(qg * (EB * 4 + 2) + eb * 4 + r) * 64] = o[qg][eb][r];
                 x[(qg * (EB * 4 + 2) + EB * 4) * 64] = negm[qg];
-                x[(qg * (EB * 4 + 2) + EB * 4 + 1) * 64] = l[qg];
+                x[(qg * (EB * 4 + 2) + EB * 4 + 1) * 64] = first_of(l[qg]);
             }
         }
         __syncthreads();
@@ -642,7 +713,7 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void k_paged_attn(AttnArgs a, Page
                 const float nm = fminf(negm[qg], nw);
                 const float a0 = fast_exp2(nm - negm[qg]), a1 = fast_exp2(nm - nw);
                 negm[qg] = nm;
-                l[qg] = l[qg] * a0 + y[(qg * (EB * 4 + 2) + EB * 4 + 1) * 64] * a1;
+                l[qg] = lsum(l[qg] * a0 + y[(qg * (EB * 4 + 2) + EB * 4 + 1) * 64] * a1);
 #pragma unroll
                 for (int eb = 0; eb < EB; ++eb)
 #pragma unroll
@@ -657,7 +728,8 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void k_paged_attn(AttnArgs a, Page
     unsigned long long again = 0;               // rows of the wave to do again
 #pragma unroll
     for (int qg = 0; qg < QG; ++qg) {
-        const float lt = quad_sum(l[qg]);
+        float lt = first_of(l[qg]);
+        if constexpr (!kOnes) lt = quad_sum(lt);
         const int r = wrow + qg * 16 + l16;
         const bool valid = r < nrows;
         if (it.splits > 1) {
@@ -680,15 +752,16 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void k_paged_attn(AttnArgs a, Page
             continue;
         }
         const float inv = 1.0f / lt;
-        bool bad = !finite(inv) || !(inv > 0.f);
+        float zero = 0.f;                       // NaN if a value is not finite
 #pragma unroll
         for (int eb = 0; eb < EB; ++eb)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 o[qg][eb][i] = keep_f32(o[qg][eb][i] * inv);
-                bad |= !finite(o[qg][eb][i]);
+                zero = fmaf(o[qg][eb][i], 0.f, zero);
             }
-        const int t = r / G, h = it.kh * G + (r - t * G);
+        const bool bad = !finite(zero) || !finite(inv) || !(inv > 0.f);
+        const int t = rows.token(r - tile0), h = it.kh * G + rows.head(r - tile0, t);
         const int64_t at = (it.row0 + t) * a.out_ld + (int64_t)h * D;
         if (valid) {
             if constexpr (kBf) {
@@ -721,9 +794,9 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void k_paged_attn(AttnArgs a, Page
         again |= ((any | any >> 16) & 0xffff) << (16 * qg);
     }
     while (again != 0) {
-        const int ri = wrow + __ffsll((long long)again) - 1, ti = ri / G;
+        const int ri = wrow - tile0 + __ffsll((long long)again) - 1, ti = rows.token(ri);
         again &= again - 1;
-        attn_row<T, D>(a, pool, it.user, n, it.row0 + ti, own ? n : pos0 + ti, it.kh * G + (ri - ti * G));
+        attn_row<T, D>(a, pool, it.user, n, it.row0 + ti, own ? n : pos0 + ti, it.kh * G + rows.head(ri, ti));
     }
 }
 
@@ -804,15 +877,10 @@ hipError_t launch_tiles(const AttnArgs& a, const PagedPool& pool, const PagedUse
 
 template <typename T, int D>
 hipError_t launch_dim(const AttnArgs& a, const PagedPool& pool, const PagedUsers& users, bool join, hipStream_t s) {
-    constexpr bool bf = sizeof(T) == 2;
-    if constexpr (D < 128)
-        if (a.tile == 16 && a.waves == 8) return launch_tiles<T, D, 1, 1, 8>(a, pool, users, join, s);
     if (a.tile == 16) return launch_tiles<T, D, 1, 1, 4>(a, pool, users, join, s);
-    if constexpr (bf) {
+    if constexpr (sizeof(T) == 2) {
         if (a.tile == 32) return launch_tiles<T, D, 2, 1, 4>(a, pool, users, join, s);
         if (a.tile == 128) return launch_tiles<T, D, 2, 4, 1>(a, pool, users, join, s);
-    } else {
-        if (a.tile == 64) return launch_tiles<T, D, 1, 4, 1>(a, pool, users, join, s);
     }
     return hipErrorInvalidValue;
 }

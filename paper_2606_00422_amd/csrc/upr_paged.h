@@ -90,10 +90,9 @@ struct AttnArgs {
     float c, ct2, cap2;             // cap2 0: none
     const float* slopes;
     int32_t window;                 // 0: none
-    // the plan: rows per tile, waves of its workgroup, keys per part (0: all),
-    // and with parts their records, `tile` per work item: [D] sums, and
-    // reference and weight sum
-    int32_t tile, waves, chunk;
+    // the plan: rows per tile, keys per part (0: all), and with parts their
+    // records, `tile` per work item: [D] sums, and reference and weight sum
+    int32_t tile, chunk;
     float* part_o;
     float* part_ml;
 };

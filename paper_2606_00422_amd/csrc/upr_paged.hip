@@ -2,7 +2,6 @@
 // and the launches of upr_rope_*, upr_paged_append and upr_paged_attention.
 #include <algorithm>
 #include <cmath>
-#include <cstdlib>
 
 #include "upr_paged_host.h"
 #include "upr_profile.h"
@@ -142,103 +141,144 @@ RopeArgs rope_args(const upr_rope* r) {
 upr_status check_model_rope(const upr_rope* r, int head_dim) { return r ? check_rope(r, head_dim) : UPR_OK; }
 
 // Cuts a call's users into launches of at most kPagedUsers and kMaxItems work
-// items; `items` gives a user's items.
+// items; `items` gives a user's items.  longest_first: in each launch, users with
+// the most cached rows first (their items take longest).
 template <typename Items, typename Launch>
-static hipError_t each_launch(const upr_segments* seg, const int32_t* rows_host, const Items& items,
-                              const Launch& launch) {
+static hipError_t each_launch(const upr_segments* seg, const int32_t* rows_host, bool longest_first,
+                              const Items& items, const Launch& launch) {
     constexpr int64_t kMaxItems = 1 << 30;
-    PagedUsers u;
-    u.n = 0;
-    u.item0[0] = 0;
-    hipError_t e = hipSuccess;
     const int32_t* const o = seg->offsets_host;
-    for (int i = 0; i < seg->num_users && e == hipSuccess; ++i) {
-        const int32_t c = o[i + 1] - o[i];
-        if (c == 0) continue;
-        const int64_t n = items(c, rows_host[i]);
-        if (n > kMaxItems) return hipErrorInvalidConfiguration;
-        if (u.n == kPagedUsers || (u.n > 0 && u.item0[u.n] + n > kMaxItems)) {
-            e = launch(u);
-            u.n = 0;
+    int32_t who[kPagedUsers];
+    int64_t total = 0;
+    int n = 0;
+    auto flush = [&]() {
+        if (longest_first)
+            std::sort(who, who + n, [&](int32_t x, int32_t y) {
+                return rows_host[x] != rows_host[y] ? rows_host[x] > rows_host[y] : x < y;
+            });
+        PagedUsers u;
+        u.n = n;
+        u.item0[0] = 0;
+        for (int i = 0; i < n; ++i) {
+            const int32_t w = who[i], c = o[w + 1] - o[w];
+            u.user[i] = w;
+            u.row0[i] = o[w];
+            u.count[i] = c;
+            u.rows[i] = rows_host[w];
+            u.item0[i + 1] = u.item0[i] + (int32_t)items(c, rows_host[w]);
         }
-        u.user[u.n] = i;
-        u.row0[u.n] = o[i];
-        u.count[u.n] = c;
-        u.rows[u.n] = rows_host[i];
-        u.item0[u.n + 1] = u.item0[u.n] + (int32_t)n;
-        ++u.n;
+        n = 0;
+        total = 0;
+        return launch(u);
+    };
+    for (int w = 0; w < seg->num_users; ++w) {
+        const int32_t c = o[w + 1] - o[w];
+        if (c == 0) continue;
+        const int64_t m = items(c, rows_host[w]);
+        if (m > kMaxItems) return hipErrorInvalidConfiguration;
+        if (n == kPagedUsers || (n > 0 && total + m > kMaxItems)) {
+            const hipError_t e = flush();
+            if (e != hipSuccess) return e;
+        }
+        who[n++] = w;
+        total += m;
     }
-    if (u.n > 0 && e == hipSuccess) e = launch(u);
-    return e;
+    return n > 0 ? flush() : hipSuccess;
 }
 
 hipError_t paged_append(int dtype, const RopeArgs& rope, const AppendArgs& a, const PagedPool& pool,
                         const upr_segments* seg, const int32_t* rows_host, hipStream_t s) {
     const int batch = append_batch(dtype, rope, a, (int64_t)seg->offsets_host[seg->num_users] - seg->offsets_host[0]);
     return each_launch(
-        seg, rows_host, [&](int32_t c, int32_t) { return append_items(dtype, rope, a, batch, c); },
+        seg, rows_host, false, [&](int32_t c, int32_t) { return append_items(dtype, rope, a, batch, c); },
         [&](const PagedUsers& u) { return launch_append(dtype, rope, a, batch, pool, u, s); });
 }
 
 // ---- the attention's plan
-static int env_int(const char* n, int d) { const char* e = getenv(n); return e ? atoi(e) : d; }
+
+// Keys that a user's rows see between them.
+static int64_t attn_keys(const AttnArgs& a, int64_t count, int32_t rows) {
+    return rows - attn_first_key(a.k_self.p ? rows : rows - (int32_t)count, a.window);
+}
 
 static int64_t attn_user_items(const AttnArgs& a, int32_t count, int32_t rows) {
     const int64_t tiles = ((int64_t)count * (a.n_heads / a.n_kv_heads) + a.tile - 1) / a.tile;
     return tiles * a.n_kv_heads * attn_splits(rows, count, a.k_self.p != nullptr, a.window, a.chunk);
 }
 
-// Tile, parts and workspace of a call, from its lengths alone.
+// Rows per tile.
+//   16: no user has more rows (or fp32, whose matrix instructions take as long
+//       per row in any tile).
+//   128: the keys of a stage serve most rows; from 192 such items up, if the
+//       tiles are at least half full.
+//   32: the rest.  Four waves share an item's keys, so that it ends sooner (4.9
+//       against 15 ns per key at head_dim 64, 8.0 against 22 at 128) and there
+//       are four times as many.
+// Measured, us, 128 / 32 rows: 4 users x 100-300 rows over 1000, 32/8 heads of
+// 128 (224 items of 128 rows): 37 / 73; 1 x 1000 over 8000, 8 heads of 64 (64
+// items): 132 / 47; 48 x 1-96 over 32-4096, window 1024 (384, a third full): 45 /
+// 34.
+static int attn_tile(int dtype, const AttnArgs& a, const upr_segments* seg) {
+    const int32_t* const o = seg->offsets_host;
+    const int64_t G = a.n_heads / a.n_kv_heads;
+    int64_t most = 0, rows = 0, tiles = 0;
+    for (int u = 0; u < seg->num_users; ++u) {
+        const int64_t r = (o[u + 1] - o[u]) * G;
+        most = std::max(most, r);
+        rows += r;
+        tiles += (r + 127) / 128;
+    }
+    if (most <= 16 || dtype == UPR_F32) return 16;
+    return tiles * a.n_kv_heads >= 192 && rows >= tiles * 64 ? 128 : 32;
+}
+
+// Keys per part, 0 for no parts.  An unsplit call takes about as long as its
+// longest item alone (tk per key) or as the device (256 CUs; cached bytes at
+// 5.2 TB/s) takes for all of them, whichever is more.  Parts pay where the item
+// is the longer by more than the join's launch; a part is then an eighth of the
+// device's time.  Long calls of single rows of 128 values, whose workgroups have
+// a CU's LDS to themselves, are cut as well until there are four per CU: nothing
+// else covers a workgroup's start there.  Measured, us, unsplit / split:
+// single rows, 8 heads of 64: one user over 1024 rows 9.3 / 9.6, 2048 13.3 /
+// 9.9, 16384 70 / 17, 16 users over 2048 15 / 23; 32/8 heads of 128: 64 users over
+// 512-16384 436 / 398.
+static int attn_chunk(int dtype, const AttnArgs& a, const upr_segments* seg, const int32_t* rows_host) {
+    const int32_t* const o = seg->offsets_host;
+    const int G = a.n_heads / a.n_kv_heads, D = a.D;
+    const double tk = 1e-3 * (dtype == UPR_F32 ? 3.0 + 0.142 * D
+                              : a.tile == 16   ? 2.6 + 0.027 * D
+                              : a.tile == 32   ? 1.8 + 0.048 * D
+                                               : 8.0 + 0.11 * D);     // us
+    double keys = 0, seen = 0, longest = 0;
+    int64_t items = 0;
+    for (int u = 0; u < seg->num_users; ++u) {
+        const int64_t c = o[u + 1] - o[u];
+        if (c == 0) continue;
+        const int64_t n = attn_keys(a, c, rows_host[u]), t = (c * G + a.tile - 1) / a.tile * a.n_kv_heads;
+        items += t;
+        keys += (double)t * n;
+        seen += (double)n * a.n_kv_heads;
+        longest = std::max(longest, (double)n);
+    }
+    const double bytes = seen * 2 * D * elem(dtype);
+    const double device = std::max({keys * tk / 256, bytes / 5.2e6, 2.0});
+    const bool even = a.tile == 16 && D == 128 && device > 60 && items < 4 * 256;
+    if (longest * tk <= device + 4 && !even) return 0;
+    double chunk = device / tk / 8;
+    if (even) chunk = std::min(chunk, keys / (4 * 256));
+    return (int)std::min<int64_t>(std::max<int64_t>(512, ((int64_t)chunk + 255) / 256 * 256), 1 << 30);
+}
+
+// Tile, parts and workspace of a call, from its lengths alone.  part_ml holds an
+// offset until the workspace is known.
 static size_t plan_attn(int dtype, AttnArgs* a, const upr_segments* seg, const int32_t* rows_host) {
     const int32_t* const o = seg->offsets_host;
-    const int G = a->n_heads / a->n_kv_heads;
-    int64_t most = 0;
-    auto items_of = [&](int tile, double* keys) {
-        int64_t items = 0;
-        *keys = 0;
-        for (int u = 0; u < seg->num_users; ++u) {
-            const int64_t c = o[u + 1] - o[u];
-            if (c == 0) continue;
-            const int64_t t = (c * G + tile - 1) / tile * a->n_kv_heads;
-            items += t;
-            *keys += (double)t * (rows_host[u] - attn_first_key(a->k_self.p ? rows_host[u] : rows_host[u] - (int)c, a->window));
-        }
-        return items;
-    };
-    for (int u = 0; u < seg->num_users; ++u) most = std::max<int64_t>(most, (int64_t)(o[u + 1] - o[u]) * G);
-    double keys = 0;
-    a->chunk = 0;
-    if (most <= 16) {
-        a->tile = 16;
-    } else if (dtype == UPR_F32) {
-        a->tile = 64;
-        if (items_of(64, &keys) < env_int("UPR_T64", 512)) a->tile = 16;
-    } else {
-        a->tile = 128;
-        if (items_of(128, &keys) < env_int("UPR_T128", 512)) a->tile = 32;
-    }
-    const int64_t items = items_of(a->tile, &keys);
-    a->waves = 4;
-    int64_t longest = 0;
-    for (int u = 0; u < seg->num_users; ++u)
-        if (o[u + 1] > o[u])
-            longest = std::max<int64_t>(longest, rows_host[u] - attn_first_key(a->k_self.p ? rows_host[u] : rows_host[u] - (o[u + 1] - o[u]), a->window));
-    if (a->tile == 16 && a->D < 128 && longest <= env_int("UPR_ALONE", 2048)) {
-        a->waves = 8;
-        return 0;
-    }
-    if (a->tile == 16 && a->D < 128) a->waves = env_int("UPR_WAVES", 4);
-    if (items > 0 && items < env_int("UPR_MAXITEMS", 1024)) {
-        // parts of equal length, whole stages, none below 512 keys
-        const double per = keys / env_int("UPR_TARGET", 1024);
-        const int64_t chunk = std::max<int64_t>(env_int("UPR_MINCHUNK", 512), ((int64_t)per + 255) / 256 * 256);
-        a->chunk = (int32_t)std::min<int64_t>(chunk, 1 << 30);
-    }
+    a->tile = attn_tile(dtype, *a, seg);
+    a->chunk = attn_chunk(dtype, *a, seg, rows_host);
     if (a->chunk == 0) return 0;
-    // launches of a call follow one another and use the same records
-    size_t bytes = 0;
+    // (launches of a call follow one another and use the same records)
     bool any = false;
-    int64_t here = 0, most_items = 0;
+    int64_t here = 0, most = 0;
     int users = 0;
     for (int u = 0; u < seg->num_users; ++u) {
         const int32_t c = o[u + 1] - o[u];
@@ -247,16 +287,15 @@ static size_t plan_attn(int dtype, AttnArgs* a, const upr_segments* seg, const i
         here += attn_user_items(*a, c, rows_host[u]);
         ++users;
         any |= attn_splits(rows_host[u], c, a->k_self.p != nullptr, a->window, a->chunk) > 1;
-        most_items = std::max(most_items, here);
+        most = std::max(most, here);
     }
     if (!any) {
         a->chunk = 0;
         return 0;
     }
-    const size_t recs = (size_t)most_items * a->tile;
-    bytes = (recs * a->D * 4 + 255) / 256 * 256;
-    a->part_ml = reinterpret_cast<float*>(bytes);       // (offset, until the workspace is known)
-    return bytes + recs * 8;
+    const size_t recs = (size_t)most * a->tile, sums = (recs * a->D * 4 + 255) / 256 * 256;
+    a->part_ml = reinterpret_cast<float*>(sums);
+    return sums + recs * 8;
 }
 
 size_t paged_attn_workspace(int dtype, const AttnArgs& args, const upr_segments* seg, const int32_t* rows_host) {
@@ -273,7 +312,7 @@ hipError_t paged_attn(int dtype, const AttnArgs& args, const PagedPool& pool, co
         a.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) + reinterpret_cast<uintptr_t>(a.part_ml));
     }
     return each_launch(
-        seg, rows_host, [&](int32_t c, int32_t n) { return attn_user_items(a, c, n); },
+        seg, rows_host, true, [&](int32_t c, int32_t n) { return attn_user_items(a, c, n); },
         [&](const PagedUsers& u) { return launch_paged_attn(dtype, a, pool, u, join, s); });
 }
 

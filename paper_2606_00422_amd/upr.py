@@ -629,9 +629,9 @@ def paged_append(cache: PagedCache, off_host, rows_host, k, v, rope=None, q=None
         pq, ldq = _rows3(q, "q", dev, dt, None, D, rows)
     if q_out is not None:
         po, ldo = (pq, ldq) if q_out is q else _rows3(q_out, "q_out", dev, dt, n_heads, D, rows)
-    status = load().upr_paged_append(upr_attn_shape(_paged_dtype(dt, "data"), n_heads, H, D), cache.view(users, layer), seg, _host_rows(rows_host, users),
-                                     rope, pk, ldk, pv, ldv, pq, ldq, po, ldo,
-                                     current_stream() if stream is None else stream)
+    shape = upr_attn_shape(_paged_dtype(dt, "data"), n_heads, H, D)
+    status = load().upr_paged_append(shape, cache.view(users, layer), seg, _host_rows(rows_host, users), rope, pk, ldk,
+                                     pv, ldv, pq, ldq, po, ldo, current_stream() if stream is None else stream)
     if status:
         _check(status)
 
@@ -684,8 +684,9 @@ def paged_attention(cache: PagedCache, off_host, rows_host, q, out=None, scale=N
     if ws is None:
         ws = paged_attention_workspace(cache, off_host, rows_host, n_heads, window, k_self is not None, stream)
     _check_flat(ws, "ws", dev, torch.uint8)
-    status = load().upr_paged_attention(upr_attn_shape(_paged_dtype(dt, "data"), n_heads, H, D), cache.view(users, layer), seg, _host_rows(rows_host, users),
-                                        opt, pq, ldq, po, ldo, ws.data_ptr(), ws.numel(),
+    shape = upr_attn_shape(_paged_dtype(dt, "data"), n_heads, H, D)
+    status = load().upr_paged_attention(shape, cache.view(users, layer), seg, _host_rows(rows_host, users), opt, pq, ldq,
+                                        po, ldo, ws.data_ptr(), ws.numel(),
                                         current_stream() if stream is None else stream)
     if status:
         _check(status)
