@@ -364,7 +364,7 @@ def test_wrappers_refuse():
     with pytest.raises(ValueError):
         upr.paged_attention(cache, offsets([4, 0]), np.asarray([20, 3], np.int32), q)     # one table
     with pytest.raises(ValueError):
-        upr.paged_attention(cache, off, pages.rows, q, slopes=torch.zeros(2, device="cuda"))
+        upr.paged_attention(cache, off, pages.rows, q, slopes=torch.zeros(2, dtype=torch.float32, device="cuda"))
     with pytest.raises(ValueError):
         upr.PagedCache(pages.data.transpose(2, 3), pages.tables_d)
     with pytest.raises(upr.UprError):

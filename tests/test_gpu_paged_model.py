@@ -49,7 +49,7 @@ def paged_run(inp, page, pieces, rope, dtype=None, seed=0):
 
 def rank_paged(inp, model, cache, rows, rope):
     C = torch.from_numpy(inp.cand_emb).cuda().to(torch.bfloat16 if inp.dtype == "bf16" else torch.float32)
-    scores = torch.full((int(inp.cand_offsets[-1]),), float("nan"), device="cuda")
+    scores = torch.full((int(inp.cand_offsets[-1]),), float("nan"), dtype=torch.float32, device="cuda")
     model.rank_paged(cache, rows, C, inp.cand_offsets, scores, rope=rope)
     torch.cuda.synchronize()
     return scores
