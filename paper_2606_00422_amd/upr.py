@@ -505,6 +505,12 @@ def _rows3(t, name, dev, like=None, heads=None, dim=None, rows=0):
     return t.data_ptr(), s0 if n > 1 else max(s0, h * d)
 
 
+def _like(t, ref) -> bool:
+    """t is laid out, typed and placed as ref, a tensor that has been checked."""
+    return type(t) is type(ref) and t.shape == ref.shape and t.stride() == ref.stride() and t.dtype == ref.dtype and \
+        t.get_device() == ref.get_device()
+
+
 def _host_rows(rows_host, users):
     if not isinstance(rows_host, np.ndarray) or rows_host.dtype != np.int32 or not rows_host.flags.c_contiguous:
         raise TypeError("rows_host must be a contiguous int32 numpy array")
@@ -545,9 +551,12 @@ def rope_apply(x, positions, rope: upr_rope, out=None, stream=None):
     rows, heads, dim = x.shape
     if out is None:
         out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    po, ldo = (px, ldx) if out is x else _rows3(out, "out", dev, x.dtype, heads, dim)
-    if out.shape[0] != rows:
-        raise ValueError("out must have x's shape")
+    if _like(out, x):
+        po, ldo = out.data_ptr(), ldx
+    else:
+        po, ldo = _rows3(out, "out", dev, x.dtype, heads, dim)
+        if out.shape[0] != rows:
+            raise ValueError("out must have x's shape")
     _check_flat(positions, "positions", dev, torch.int32)
     if positions.dim() != 1 or positions.shape[0] != rows:
         raise ValueError("positions must be [rows]")
@@ -595,16 +604,18 @@ class PagedCache:
     def view(self, users: int, layer=None) -> upr_paged_cache:
         """The C struct, of one layer's plane or (None) of the whole pool."""
         data, tables = self.data, self.tables
-        _check_here(data, "the cache")
+        if data.get_device() != _device():
+            raise ValueError(f"the cache is on {data.device}, the current device is cuda:{_device()}")
+        shape = data.shape
         held, width = tables.shape
         if held < users:
             raise ValueError(f"tables has {held} users, {users} needed")
-        shape = data.shape
         at = data.data_ptr()
-        if layer is not None and not 0 <= layer < (shape[0] if len(shape) == 6 else 1):
-            raise ValueError(f"the cache has no layer {layer}")
-        if layer:
-            at += layer * data.stride(0) * data.element_size()
+        if layer is not None:
+            if not 0 <= layer < (shape[0] if len(shape) == 6 else 1):
+                raise ValueError(f"the cache has no layer {layer}")
+            if layer:
+                at += layer * data.stride(0) * data.element_size()
         return upr_paged_cache(at, shape[-5], shape[-2], width, tables.data_ptr())
 
 
@@ -622,13 +633,14 @@ def paged_append(cache: PagedCache, off_host, rows_host, k, v, rope=None, q=None
     users, rows = seg.num_users, int(off_host[-1])
     H, D, dt = cache.heads()
     pk, ldk = _rows3(k, "k", dev, dt, H, D, rows)
-    pv, ldv = _rows3(v, "v", dev, dt, H, D, rows)
+    pv, ldv = (v.data_ptr(), ldk) if _like(v, k) else _rows3(v, "v", dev, dt, H, D, rows)
     n_heads, pq, ldq, po, ldo = H, None, 0, None, 0
     if q is not None:
         n_heads = q.shape[1]
         pq, ldq = _rows3(q, "q", dev, dt, None, D, rows)
     if q_out is not None:
-        po, ldo = (pq, ldq) if q_out is q else _rows3(q_out, "q_out", dev, dt, n_heads, D, rows)
+        same = q is not None and _like(q_out, q)
+        po, ldo = (q_out.data_ptr(), ldq) if same else _rows3(q_out, "q_out", dev, dt, n_heads, D, rows)
     shape = upr_attn_shape(_paged_dtype(dt, "data"), n_heads, H, D)
     status = load().upr_paged_append(shape, cache.view(users, layer), seg, _host_rows(rows_host, users), rope, pk, ldk,
                                      pv, ldv, pq, ldq, po, ldo, current_stream() if stream is None else stream)
@@ -668,7 +680,7 @@ def paged_attention(cache: PagedCache, off_host, rows_host, q, out=None, scale=N
     n_heads = q.shape[1]
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    po, ldo = _rows3(out, "out", dev, dt, n_heads, D, rows)
+    po, ldo = (out.data_ptr(), ldq) if _like(out, q) else _rows3(out, "out", dev, dt, n_heads, D, rows)
     if slopes is not None:
         _check_flat(slopes, "slopes", dev, torch.float32)
         if tuple(slopes.shape) != (n_heads,):
@@ -677,7 +689,8 @@ def paged_attention(cache: PagedCache, off_host, rows_host, q, out=None, scale=N
     if k_self is not None:
         pks, lds = _rows3(k_self, "k_self", dev, dt, H, D, rows)
     if v_self is not None:
-        pvs, ldv = _rows3(v_self, "v_self", dev, dt, H, D, rows)
+        same = k_self is not None and _like(v_self, k_self)
+        pvs, ldv = (v_self.data_ptr(), lds) if same else _rows3(v_self, "v_self", dev, dt, H, D, rows)
         if k_self is not None and ldv != lds:
             raise ValueError("k_self and v_self must have the same row stride")
     opt = _attn_options(scale, softcap, window, slopes, D, pks, pvs, lds)
