@@ -278,9 +278,12 @@ __global__ __launch_bounds__(64 * RW * KW, RW > 1 && D < 128 ? (EX ? 3 : 4) : 2)
     // not queue behind the stages')
     typedef const __attribute__((address_space(4))) int32_t* constants;
     const constants table = (constants)(uintptr_t)(pool.tables + (int64_t)it.user * pool.stride);
-    const int64_t block = (int64_t)pool.page_rows * D * (int)sizeof(T);     // one head's rows of a page
+    // (one page's bytes: at most 2 x 1024 heads x 1024 rows x 512 bytes)
+    constexpr int RB = D * (int)sizeof(T);
+    const uint32_t v_off = (uint32_t)a.n_kv_heads * pool.page_rows * RB, page_bytes = 2 * v_off;
+    const char* const head0 = pool.data + (size_t)((uint32_t)it.kh * pool.page_rows * RB);
     const int rbase = wave * RPW;
-    int offK[8], offV[8];
+    int offK[8], offV[8];       // (fixed size: with a template-dependent one the host pass drops the launch stub)
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
         const int row = rbase + i * RPL + lane / CR, slot = lane % CR;
@@ -288,32 +291,36 @@ __global__ __launch_bounds__(64 * RW * KW, RW > 1 && D < 128 ? (EX ? 3 : 4) : 2)
         offK[i] = r16 * D * (int)sizeof(T) + ((slot ^ key_k<T, D>(row)) << 4);
         offV[i] = r16 * D * (int)sizeof(T) + ((slot ^ key_v<T, D>(row)) << 4);
     }
-    // page numbers of a stage's pieces (a piece never crosses a page)
-    int pid[4];
+    // A wave's rows of a stage are pieces of 16, which never cross a page; pages
+    // of 32 rows and more hold two of them (stages start at multiples of 32).
+    const bool pairs = pool.page_rows >= 32;
+    int pid[4];                 // page numbers of the pieces
     auto fetch_pages = [&](int st) __attribute__((always_inline)) {
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
             const int key = k0 + st * TS + rbase + 16 * p;
+            if (p % 2 == 1 && pairs) continue;
             pid[p] = key < n ? table[key >> pool.page_shift] : -1;
         }
     };
     auto issue_loads = [&](T* dK, T* dV, int st) __attribute__((always_inline)) {
+        const char* pk = head0;
+        int bytes = 0, base = 0;
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
             const int key = k0 + st * TS + rbase + 16 * p;
-            const int base = key & -pool.page_rows;
-            // rows of the page that hold keys; none past the last key or in a
-            // page outside the pool
-            const int page = pid[p];
-            const bool in = page >= 0 && page < pool.n_pages;
-            const int rest = n - base < pool.page_rows ? n - base : pool.page_rows;
-            const int valid = in ? rest : 0;
-            char* const pk = pool.data + ((int64_t)(in ? page : 0) * 2 * a.n_kv_heads + it.kh) * block;
-            const __amdgpu_buffer_rsrc_t rsK =
-                __builtin_amdgcn_make_buffer_rsrc(pk, (short)0, valid * D * (int)sizeof(T), 0x00020000);
-            const __amdgpu_buffer_rsrc_t rsV = __builtin_amdgcn_make_buffer_rsrc(
-                pk + a.n_kv_heads * block, (short)0, valid * D * (int)sizeof(T), 0x00020000);
-            const int off = (key - base) * D * (int)sizeof(T);
+            if (p % 2 == 0 || !pairs) {
+                base = key & -pool.page_rows;
+                // rows of the page that hold keys; none past the last key or in
+                // a page outside the pool
+                const bool in = (uint32_t)pid[p] < (uint32_t)pool.n_pages;
+                bytes = in ? (n - base < pool.page_rows ? n - base : pool.page_rows) * RB : 0;
+                pk = head0 + (uint64_t)(in ? (uint32_t)pid[p] : 0u) * page_bytes;
+            }
+            const __amdgpu_buffer_rsrc_t rsK = __builtin_amdgcn_make_buffer_rsrc((void*)pk, (short)0, bytes, 0x00020000);
+            const __amdgpu_buffer_rsrc_t rsV =
+                __builtin_amdgcn_make_buffer_rsrc((void*)(pk + v_off), (short)0, bytes, 0x00020000);
+            const int off = (key - base) * RB;
 #pragma unroll
             for (int i = 0; i < NI; ++i) {
                 if (i * RPL / 16 != p) continue;
@@ -800,103 +807,117 @@ __global__ __launch_bounds__(64 * RW * KW, RW > 1 && D < 128 ? (EX ? 3 : 4) : 2)
     }
 }
 
-// Joins the parts of the rows whose keys were split: one wave per row.  Part
-// records of item b (its tile and key/value head, part 0) follow those of the
-// next part n_kv_heads items on.
-template <typename T, int D, int TR>
-__global__ __launch_bounds__(256) void k_paged_attn_join(AttnArgs a, PagedPool pool, PagedUsers users) {
-    const Item it = find_item<TR>(a, users, blockIdx.x);
-    if (it.splits == 1 || it.split != 0) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int G = a.n_heads / a.n_kv_heads, nrows = it.count * G, tile0 = it.tile * TR;
-    const int here = nrows - tile0 < TR ? nrows - tile0 : TR;
-    constexpr int kE = D > 64 ? D / 64 : 1;
+// Joins the parts of the rows whose keys were split: one wave per row.  The
+// records of a tile's part are those of the attention's item ((tile * parts +
+// part) * n_kv_heads + head) of its user.
+template <typename T, int D>
+__global__ __launch_bounds__(64 * kJoinRows) void k_paged_attn_join(AttnArgs a, PagedPool pool, JoinUsers join) {
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const PagedUsers& users = join.users;
+    const int i = user_of(users, blockIdx.x);
+    const int idx = (int)blockIdx.x - users.item0[i], group = idx / a.n_kv_heads, kh = idx - group * a.n_kv_heads;
+    const bool own = a.k_self.p != nullptr;
+    const int n = users.rows[i], count = users.count[i];
+    const int G = a.n_heads / a.n_kv_heads, nrows = count * G;
+    const int r = group * kJoinRows + wave;
+    if (r >= nrows) return;
+    const int splits = attn_splits(n, count, own, a.window, a.chunk);
+    int tile = r / a.tile;
+    const int in_tile = r - tile * a.tile;
+    if (!own) tile = (nrows + a.tile - 1) / a.tile - 1 - tile;      // (last tiles first)
+    const int64_t step = (int64_t)a.n_kv_heads * a.tile;
+    const int64_t rec0 = ((int64_t)join.part0[i] + (int64_t)tile * splits * a.n_kv_heads + kh) * a.tile + in_tile;
     // lane j of part s: values E j .. E j + E - 1, of every PP-th part
     constexpr int E = D / 32, PP = 2;
     typedef __attribute__((ext_vector_type(E))) float part;
     const int e0 = (lane & 31) * E, half = lane >> 5;
-    for (int i = wave; i < here; i += 4) {
-        const int64_t rec0 = (int64_t)blockIdx.x * TR + i, step = (int64_t)a.n_kv_heads * TR;
-        float nm = -kUnset, l = 0.f, acc[E];
+    float nm = -kUnset, l = 0.f, acc[E];
 #pragma unroll
-        for (int j = 0; j < E; ++j) acc[j] = 0.f;
-        for (int s0 = 0; s0 < it.splits; s0 += 64) {
-            // 64 parts' references and sums, one per lane
-            const int left = it.splits - s0 < 64 ? it.splits - s0 : 64;
-            const int64_t rs = rec0 + (int64_t)(s0 + (lane < left ? lane : 0)) * step;
-            const float ns = lane < left ? a.part_ml[2 * rs] : -kUnset;
-            const float ls = lane < left ? a.part_ml[2 * rs + 1] : 0.f;
-            const float nn = fminf(nm, -wave_max(-ns));
-            const float alpha = fast_exp2(nn - nm), w = fast_exp2(nn - ns);
-            nm = nn;
-            l = l * alpha + wave_sum(w * ls);
+    for (int j = 0; j < E; ++j) acc[j] = 0.f;
+    for (int s0 = 0; s0 < splits; s0 += 64) {
+        // 64 parts' references and sums, one per lane
+        const int left = splits - s0 < 64 ? splits - s0 : 64;
+        const int64_t rs = rec0 + (int64_t)(s0 + (lane < left ? lane : 0)) * step;
+        const float ns = lane < left ? a.part_ml[2 * rs] : -kUnset;
+        const float ls = lane < left ? a.part_ml[2 * rs + 1] : 0.f;
+        const float nn = fminf(nm, -wave_max(-ns));
+        const float alpha = fast_exp2(nn - nm), w = fast_exp2(nn - ns);
+        nm = nn;
+        l = l * alpha + wave_sum(w * ls);
 #pragma unroll
-            for (int j = 0; j < E; ++j) acc[j] *= alpha;
-            // their outputs, PP at a time, eight loads under way
+        for (int j = 0; j < E; ++j) acc[j] *= alpha;
+        // their outputs, PP at a time, eight loads under way
 #pragma unroll 8
-            for (int s = 0; s < left; s += PP) {
-                const int mine = s + half < left ? s + half : s;
-                const part v = *reinterpret_cast<const part*>(a.part_o + (rec0 + (int64_t)(s0 + mine) * step) * D + e0);
-                const float ws = s + half < left ? __shfl(w, mine, 64) : 0.f;
+        for (int s = 0; s < left; s += PP) {
+            const int mine = s + half < left ? s + half : s;
+            const part v = *reinterpret_cast<const part*>(a.part_o + (rec0 + (int64_t)(s0 + mine) * step) * D + e0);
+            const float ws = s + half < left ? __shfl(w, mine, 64) : 0.f;
 #pragma unroll
-                for (int j = 0; j < E; ++j) acc[j] = fmaf(ws, v[j], acc[j]);
-            }
+            for (int j = 0; j < E; ++j) acc[j] = fmaf(ws, v[j], acc[j]);
         }
-#pragma unroll
-        for (int j = 0; j < E; ++j) acc[j] += __shfl_xor(acc[j], 32, 64);
-        const float inv = 1.f / l;
-        bool bad = !finite(inv) || !(inv > 0.f);
-        const int r = tile0 + i, t = r / G, h = it.kh * G + (r - t * G);
-        const int64_t row = it.row0 + t, at = row * a.out_ld + (int64_t)h * D + e0;
-#pragma unroll
-        for (int j = 0; j < E; ++j) {
-            const float v = keep_f32(acc[j] * inv);
-            bad |= !finite(v);
-            if (half) continue;
-            if (a.out_kind == ATTN_OUT_F16) static_cast<f16*>(a.out)[at + j] = (f16)v;
-            else if (a.out_kind == ATTN_OUT_F32) static_cast<float*>(a.out)[at + j] = v;
-            else static_cast<T*>(a.out)[at + j] = (T)v;
-        }
-        if (__any(bad))
-            attn_row<T, D>(a, pool, it.user, it.rows, row, a.k_self.p != nullptr ? it.rows : it.rows - it.count + t, h);
     }
+#pragma unroll
+    for (int j = 0; j < E; ++j) acc[j] += __shfl_xor(acc[j], 32, 64);
+    const float inv = 1.f / l;
+    bool bad = !finite(inv) || !(inv > 0.f);
+    const int t = r / G, h = kh * G + (r - t * G);
+    const int64_t row = (int64_t)users.row0[i] + t, at = row * a.out_ld + (int64_t)h * D + e0;
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+        const float v = keep_f32(acc[j] * inv);
+        bad |= !finite(v);
+        if (half) continue;
+        if (a.out_kind == ATTN_OUT_F16) static_cast<f16*>(a.out)[at + j] = (f16)v;
+        else if (a.out_kind == ATTN_OUT_F32) static_cast<float*>(a.out)[at + j] = v;
+        else static_cast<T*>(a.out)[at + j] = (T)v;
+    }
+    if (__any(bad)) attn_row<T, D>(a, pool, users.user[i], n, row, own ? n : n - count + t, h);
 }
 
 template <typename T, int D, int QG, int RW, int KW>
-hipError_t launch_tiles(const AttnArgs& a, const PagedPool& pool, const PagedUsers& users, bool join, hipStream_t s) {
+void launch_tiles(const AttnArgs& a, const PagedPool& pool, const PagedUsers& users, hipStream_t s) {
     const unsigned grid = (unsigned)users.item0[users.n];
     if (a.cap2 > 0.f || a.slopes != nullptr)
         k_paged_attn<T, D, QG, RW, KW, true><<<grid, 64 * RW * KW, 0, s>>>(a, pool, users);
     else
         k_paged_attn<T, D, QG, RW, KW, false><<<grid, 64 * RW * KW, 0, s>>>(a, pool, users);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || !join) return e;
-    k_paged_attn_join<T, D, 16 * QG * RW><<<grid, 256, 0, s>>>(a, pool, users);
-    return hipGetLastError();
 }
 
-template <typename T, int D>
-hipError_t launch_dim(const AttnArgs& a, const PagedPool& pool, const PagedUsers& users, bool join, hipStream_t s) {
-    if (a.tile == 16) return launch_tiles<T, D, 1, 1, 4>(a, pool, users, join, s);
-    if constexpr (sizeof(T) == 2) {
-        if (a.tile == 32) return launch_tiles<T, D, 2, 1, 4>(a, pool, users, join, s);
-        if (a.tile == 128) return launch_tiles<T, D, 2, 4, 1>(a, pool, users, join, s);
-    }
-    return hipErrorInvalidValue;
+// go(type, head_dim) of a call.
+template <typename Go>
+void with_type_and_dim(int dtype, int D, const Go& go) {
+    auto at = [&](auto t) {
+        if (D == 32) go(t, std::integral_constant<int, 32>{});
+        else if (D == 64) go(t, std::integral_constant<int, 64>{});
+        else go(t, std::integral_constant<int, 128>{});
+    };
+    if (dtype == UPR_F32) at(float{}); else at(bf16{});
 }
 
 }  // namespace
 
-hipError_t launch_paged_attn(int dtype, const AttnArgs& a, const PagedPool& pool, const PagedUsers& users, bool join,
+hipError_t launch_paged_attn(int dtype, const AttnArgs& a, const PagedPool& pool, const PagedUsers& users,
                              hipStream_t s) {
     if (users.item0[users.n] == 0) return hipSuccess;
-    auto go = [&](auto t) {
+    with_type_and_dim(dtype, a.D, [&](auto t, auto d) {
         typedef decltype(t) T;
-        if (a.D == 32) return launch_dim<T, 32>(a, pool, users, join, s);
-        if (a.D == 64) return launch_dim<T, 64>(a, pool, users, join, s);
-        return launch_dim<T, 128>(a, pool, users, join, s);
-    };
-    return dtype == UPR_F32 ? go(float{}) : go(bf16{});
+        constexpr int D = decltype(d)::value;
+        if constexpr (sizeof(T) == 2) {
+            if (a.tile == 32) return launch_tiles<T, D, 2, 1, 4>(a, pool, users, s);
+            if (a.tile == 128) return launch_tiles<T, D, 2, 4, 1>(a, pool, users, s);
+        }
+        launch_tiles<T, D, 1, 1, 4>(a, pool, users, s);
+    });
+    return hipGetLastError();
+}
+
+hipError_t launch_paged_join(int dtype, const AttnArgs& a, const PagedPool& pool, const JoinUsers& join, hipStream_t s) {
+    with_type_and_dim(dtype, a.D, [&](auto t, auto d) {
+        k_paged_attn_join<decltype(t), decltype(d)::value>
+            <<<(unsigned)join.users.item0[join.users.n], 64 * kJoinRows, 0, s>>>(a, pool, join);
+    });
+    return hipGetLastError();
 }
 
 }  // namespace upr

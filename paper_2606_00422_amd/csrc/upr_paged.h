@@ -96,7 +96,16 @@ struct AttnArgs {
     float* part_o;
     float* part_ml;
 };
-hipError_t launch_paged_attn(int dtype, const AttnArgs& a, const PagedPool& pool, const PagedUsers& users, bool join,
+hipError_t launch_paged_attn(int dtype, const AttnArgs& a, const PagedPool& pool, const PagedUsers& users,
                              hipStream_t s);
+
+// Join of a launch's parts.  users: those of the attention's launch with parts,
+// items of kJoinRows rows of one key/value head; part0: their first item there.
+constexpr int kJoinRows = 4;
+struct JoinUsers {
+    PagedUsers users;
+    int32_t part0[kPagedUsers];
+};
+hipError_t launch_paged_join(int dtype, const AttnArgs& a, const PagedPool& pool, const JoinUsers& join, hipStream_t s);
 
 }  // namespace upr

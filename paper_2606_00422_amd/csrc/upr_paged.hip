@@ -311,9 +311,29 @@ hipError_t paged_attn(int dtype, const AttnArgs& args, const PagedPool& pool, co
         a.part_o = static_cast<float*>(ws);
         a.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) + reinterpret_cast<uintptr_t>(a.part_ml));
     }
+    const int G = a.n_heads / a.n_kv_heads;
     return each_launch(
         seg, rows_host, true, [&](int32_t c, int32_t n) { return attn_user_items(a, c, n); },
-        [&](const PagedUsers& u) { return launch_paged_attn(dtype, a, pool, u, join, s); });
+        [&](const PagedUsers& u) {
+            const hipError_t e = launch_paged_attn(dtype, a, pool, u, s);
+            if (e != hipSuccess || !join) return e;
+            JoinUsers j;
+            j.users.n = 0;
+            j.users.item0[0] = 0;
+            for (int i = 0; i < u.n; ++i) {
+                if (attn_splits(u.rows[i], u.count[i], a.k_self.p != nullptr, a.window, a.chunk) == 1) continue;
+                const int k = j.users.n++;
+                j.users.user[k] = u.user[i];
+                j.users.row0[k] = u.row0[i];
+                j.users.count[k] = u.count[i];
+                j.users.rows[k] = u.rows[i];
+                j.part0[k] = u.item0[i];
+                // (at most the rows of the parts' records: no more than items * tile)
+                const int64_t groups = ((int64_t)u.count[i] * G + kJoinRows - 1) / kJoinRows * a.n_kv_heads;
+                j.users.item0[k + 1] = j.users.item0[k] + (int32_t)groups;
+            }
+            return j.users.n > 0 ? launch_paged_join(dtype, a, pool, j, s) : e;
+        });
 }
 
 }  // namespace upr
