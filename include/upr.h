@@ -427,7 +427,8 @@ upr_status upr_mx_linear(const uint8_t* a_codes, const uint8_t* a_scales, const 
  *     rows are part of it; UPR_ERR_CAPACITY: the table has fewer than
  *     ceil(rows_host[u] / page_rows) entries per user; UPR_ERR_LIMIT:
  *     page_rows not a power of two in [16, 1024], rows_host[u] above 2^30,
- *     a leading dimension too small, or a buffer or leading dimension that is
+ *     more than 2^22 rows of a user in one call or 2^27 with their heads, a
+ *     leading dimension too small, or a buffer or leading dimension that is
  *     not a multiple of 16 bytes; UPR_ERR_CONFIG: an unsupported shape.
  *   - Leading dimensions (`_ld`) count elements between consecutive rows; a
  *     row holds its heads one after the other.  Row r of a buffer is the
@@ -503,8 +504,8 @@ upr_status upr_rope_apply(const upr_rope* rope, int32_t dtype, int32_t heads, in
 /* Writes the keys k and values v of the new rows into the pages, the keys
  * rotated at their positions when rope is given (NULL: as they are).  With q,
  * the queries of the same rows go to q_out likewise (rotated, or copied
- * without rope; q_out may be q with the same leading dimension); q and q_out
- * are both NULL or both given.  Only the new rows' places in the pages are
+ * without rope; q_out may be q with the same leading dimension, and must not
+ * overlap k, v or the pages otherwise); q and q_out are both NULL or both given.  Only the new rows' places in the pages are
  * written; two new rows of one call must not share a place.  Allocates nothing. */
 upr_status upr_paged_append(const upr_attn_shape* shape, const upr_paged_cache* cache, const upr_segments* fresh,
                             const int32_t* rows_host, const upr_rope* rope, const void* k, int64_t k_ld,

@@ -300,7 +300,7 @@ __global__ __launch_bounds__(64 * RW * KW, RW > 1 && D < 128 ? (EX ? 3 : 4) : 2)
         for (int p = 0; p < NP; ++p) {
             const int key = k0 + st * TS + rbase + 16 * p;
             if (p % 2 == 1 && pairs) continue;
-            pid[p] = key < n ? table[key >> pool.page_shift] : -1;
+            pid[p] = key < k1 ? table[key >> pool.page_shift] : -1;
         }
     };
     auto issue_loads = [&](T* dK, T* dV, int st) __attribute__((always_inline)) {
@@ -311,8 +311,8 @@ __global__ __launch_bounds__(64 * RW * KW, RW > 1 && D < 128 ? (EX ? 3 : 4) : 2)
             const int key = k0 + st * TS + rbase + 16 * p;
             if (p % 2 == 0 || !pairs) {
                 base = key & -pool.page_rows;
-                // rows of the page that hold keys; none past the last key or in
-                // a page outside the pool
+                // rows of the page that hold keys; none past this part's keys or
+                // in a page outside the pool
                 const bool in = (uint32_t)pid[p] < (uint32_t)pool.n_pages;
                 bytes = in ? (n - base < pool.page_rows ? n - base : pool.page_rows) * RB : 0;
                 pk = head0 + (uint64_t)(in ? (uint32_t)pid[p] : 0u) * page_bytes;

@@ -193,8 +193,13 @@ hipError_t launch_rope(int dtype, const RopeArgs& rope, int heads, int D, RowsOf
     const int64_t per = split_row(vec, batch, heads, D).rows;
     with_types(dtype, vec, batch, [&](auto t, auto v, auto b) {
         typedef decltype(t) T;
-        k_rope<T, decltype(v)::value, decltype(b)::value><<<(unsigned)((rows + per - 1) / per), 256, 0, s>>>(
-            rope, heads, D, static_cast<const T*>(x.p), x.ld, positions, rows, static_cast<T*>(out), out_ld);
+        const int64_t most = (int64_t{1} << 23) * per;      // (a launch has fewer than 2^32 threads)
+        for (int64_t r0 = 0; r0 < rows; r0 += most) {
+            const int64_t n = rows - r0 < most ? rows - r0 : most;
+            k_rope<T, decltype(v)::value, decltype(b)::value><<<(unsigned)((n + per - 1) / per), 256, 0, s>>>(
+                rope, heads, D, static_cast<const T*>(x.p) + r0 * x.ld, x.ld, positions + r0, n,
+                static_cast<T*>(out) + r0 * out_ld, out_ld);
+        }
     });
     return hipGetLastError();
 }

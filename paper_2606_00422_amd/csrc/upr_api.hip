@@ -1296,7 +1296,8 @@ static upr_status paged_plan(const upr_model* m, const upr_paged_cache* cache, c
     upr_status st = upr::check_paged_cache(cache, false);
     int64_t rows = 0;
     if (st == UPR_OK)
-        st = upr::check_paged_users(seg, name, rows_host, cache->page_rows, cache->table_stride, !own, &rows);
+        st = upr::check_paged_users(seg, name, rows_host, cache->page_rows, cache->table_stride, m->cfg.n_heads, !own,
+                                    &rows);
     if (st == UPR_OK) st = upr::check_model_rope(rope, m->cfg.head_dim);
     if (st != UPR_OK) return st;
     upr::AttnArgs a{};

@@ -11,6 +11,9 @@ namespace upr {
 namespace {
 
 constexpr int32_t kMaxRows = 1 << 30;
+// (a launch has fewer than 2^32 threads: one user's work items have to fit)
+constexpr int32_t kMaxCount = 1 << 22;
+constexpr int64_t kMaxCountHeads = int64_t{1} << 27;
 
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
@@ -72,7 +75,7 @@ upr_status check_page_rows(int32_t page_rows) {
 }
 
 upr_status check_paged_users(const upr_segments* seg, const char* name, const int32_t* rows_host, int32_t page_rows,
-                             int32_t table_stride, bool part_of_cache, int64_t* total) {
+                             int32_t table_stride, int n_heads, bool part_of_cache, int64_t* total) {
     if (!seg) return report_error(UPR_ERR_NULL, "%s segments pointer is NULL", name);
     if (seg->num_users < 0) return report_error(UPR_ERR_OFFSETS, "%s num_users %d < 0", name, seg->num_users);
     if (!seg->offsets_host) return report_error(UPR_ERR_NULL, "%s offsets_host is NULL", name);
@@ -86,6 +89,9 @@ upr_status check_paged_users(const upr_segments* seg, const char* name, const in
         if (n < 0 || (part_of_cache && n < c))
             return report_error(UPR_ERR_OFFSETS, "user %d has %d cached rows, %d of them new", u, n, c);
         if (n > kMaxRows) return report_error(UPR_ERR_LIMIT, "user %d has %d cached rows (at most %d)", u, n, kMaxRows);
+        if (c > kMaxCount || (int64_t)c * n_heads > kMaxCountHeads)
+            return report_error(UPR_ERR_LIMIT, "user %d has %d rows of %d heads (at most 2^22, and 2^27 with the heads)",
+                                u, c, n_heads);
         if (c > 0 && ((int64_t)n + page_rows - 1) / page_rows > table_stride)
             return report_error(UPR_ERR_CAPACITY, "user %d has %d cached rows, its table %d pages of %d", u, n,
                                 table_stride, page_rows);
@@ -146,7 +152,7 @@ upr_status check_model_rope(const upr_rope* r, int head_dim) { return r ? check_
 template <typename Items, typename Launch>
 static hipError_t each_launch(const upr_segments* seg, const int32_t* rows_host, bool longest_first,
                               const Items& items, const Launch& launch) {
-    constexpr int64_t kMaxItems = 1 << 30;
+    constexpr int64_t kMaxItems = 1 << 23;      // of 256 threads
     const int32_t* const o = seg->offsets_host;
     int32_t who[kPagedUsers];
     int64_t total = 0;
@@ -433,7 +439,8 @@ upr_status upr_paged_append(const upr_attn_shape* shape, const upr_paged_cache* 
     if (st == UPR_OK) st = check_paged_cache(cache, false);
     int64_t rows = 0;
     if (st == UPR_OK)
-        st = check_paged_users(fresh, "fresh", rows_host, cache->page_rows, cache->table_stride, true, &rows);
+        st = check_paged_users(fresh, "fresh", rows_host, cache->page_rows, cache->table_stride, shape->n_heads, true,
+                               &rows);
     if (st == UPR_OK && rope) st = check_rope(rope, shape->head_dim);
     if (st != UPR_OK) return st;
     if ((q == nullptr) != (q_out == nullptr))
@@ -474,8 +481,8 @@ size_t upr_paged_attention_workspace_bytes(const upr_attn_shape* shape, const up
     int64_t rows;
     if (check_shape(shape) != UPR_OK || check_paged_cache(cache, false) != UPR_OK ||
         check_attn_options(options) != UPR_OK ||
-        check_paged_users(queries, "query", rows_host, cache->page_rows, cache->table_stride, !options->k_self,
-                          &rows) != UPR_OK)
+        check_paged_users(queries, "query", rows_host, cache->page_rows, cache->table_stride, shape->n_heads,
+                          !options->k_self, &rows) != UPR_OK)
         return 0;
     return paged_attn_workspace(shape->dtype, attn_args(*shape, *options), queries, rows_host);
 }
@@ -489,8 +496,8 @@ upr_status upr_paged_attention(const upr_attn_shape* shape, const upr_paged_cach
     if (st == UPR_OK) st = check_attn_options(options);
     int64_t rows = 0;
     if (st == UPR_OK)
-        st = check_paged_users(queries, "query", rows_host, cache->page_rows, cache->table_stride, !options->k_self,
-                               &rows);
+        st = check_paged_users(queries, "query", rows_host, cache->page_rows, cache->table_stride, shape->n_heads,
+                               !options->k_self, &rows);
     if (st != UPR_OK) return st;
     if (rows == 0) return report_ok();
     const int D = shape->head_dim, dt = shape->dtype;

@@ -12,7 +12,7 @@ namespace upr {
 upr_status check_page_rows(int32_t page_rows);
 upr_status check_paged_cache(const upr_paged_cache* c, bool pointers);
 upr_status check_paged_users(const upr_segments* seg, const char* name, const int32_t* rows_host, int32_t page_rows,
-                             int32_t table_stride, bool part_of_cache, int64_t* total);
+                             int32_t table_stride, int n_heads, bool part_of_cache, int64_t* total);
 upr_status check_model_rope(const upr_rope* r, int head_dim);
 
 PagedPool paged_pool(const upr_paged_cache& c, size_t plane_bytes, int plane);

@@ -141,6 +141,8 @@ COMMON = [
     (dict(seg__num_users=-1), upr.UPR_ERR_OFFSETS), (dict(rows=(5, -1, 40)), upr.UPR_ERR_OFFSETS),
     (dict(rows=(1, 9, 40)), upr.UPR_ERR_OFFSETS), (dict(counts=(2, -1, 3)), upr.UPR_ERR_OFFSETS),
     (dict(rows=(5, 9, (1 << 30) + 1)), upr.UPR_ERR_LIMIT),
+    (dict(counts=((1 << 22) + 1, 0, 3), rows=(1 << 23, 9, 40), cache__table_stride=1 << 20), upr.UPR_ERR_LIMIT),
+    (dict(counts=(1 << 20, 0, 3), rows=(1 << 20, 9, 40), cache__table_stride=1 << 20, shape__n_heads=256), upr.UPR_ERR_LIMIT),
     (dict(cache__data=None), upr.UPR_ERR_NULL), (dict(cache__tables=None), upr.UPR_ERR_NULL),
     (dict(cache__data=A + 4), upr.UPR_ERR_LIMIT),
     (dict(p__q=A + 2), upr.UPR_ERR_LIMIT), (dict(p__q_ld=511), upr.UPR_ERR_LIMIT), (dict(p__q_ld=516), upr.UPR_ERR_LIMIT),
