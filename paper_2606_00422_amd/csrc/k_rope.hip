@@ -212,9 +212,8 @@ int append_batch(int dtype, const RopeArgs& rope, const AppendArgs& a, int64_t r
     return batch_of(rows, append_heads(a), a.D, vec_of(dtype, rope));
 }
 
-int64_t append_items(int dtype, const RopeArgs& rope, const AppendArgs& a, int batch, int64_t count) {
-    const int64_t per = split_row(vec_of(dtype, rope), batch, append_heads(a), a.D).rows;
-    return (count + per - 1) / per;
+int append_rows(int dtype, const RopeArgs& rope, const AppendArgs& a, int batch) {
+    return split_row(vec_of(dtype, rope), batch, append_heads(a), a.D).rows;
 }
 
 hipError_t launch_append(int dtype, const RopeArgs& rope, const AppendArgs& a, int batch, const PagedPool& pool,

@@ -394,20 +394,20 @@ struct PagedCall {
     const int32_t* rows_host;
     RopeArgs rope;              // rot_dim 0: no positions
     size_t plane_bytes;
+    AttnArgs plan;              // the attention's plan, its pointers left open
 };
 
 // Attention of the q|k|v rows of one layer over its plane of pages -> o
 // (`kind`).  Queries carry log2(e)/sqrt(D) already.  own: candidates, each with
 // its own key and value; else the rows are the newest of the cache.
-static AttnArgs paged_attn_args(const upr_config& c, const void* qkv, int64_t row0, void* o, int kind, bool own) {
+static AttnArgs paged_attn_args(const upr_config& c, const AttnArgs& plan, const void* qkv, int64_t row0, void* o, int kind,
+                                bool own) {
     const int d = c.d_model;
     // rows of the workspace start at the call's first row
     auto rows = [&](const void* p, int64_t ld, size_t es) { return static_cast<const char*>(p) - (size_t)row0 * ld * es; };
     const size_t es = elem_size(c), o_es = kind == ATTN_OUT_F16 ? 2 : kind == ATTN_OUT_F32 ? 4 : es;
     const char* const q = rows(qkv, 3 * d, es);
-    AttnArgs a{};
-    a.n_heads = a.n_kv_heads = c.n_heads;
-    a.D = c.head_dim;
+    AttnArgs a = plan;
     a.q = RowsOf{q, 3 * d};
     if (own) {
         a.k_self = RowsOf{q + d * es, 3 * d};
@@ -427,7 +427,7 @@ static int paged_dtype(const upr_config& c) { return bf16_family(c.dtype) ? UPR_
 static hipError_t rank_attn_paged(const upr_config& c, const PagedCall& pc, const upr_segments* cand, int layer,
                                   void* qkv, int64_t row0, void* o, int kind, void* ws, hipStream_t s) {
     const PagedPool pool = paged_pool(*pc.cache, pc.plane_bytes, layer);
-    const AttnArgs a = paged_attn_args(c, qkv, row0, o, kind, true);
+    const AttnArgs a = paged_attn_args(c, pc.plan, qkv, row0, o, kind, true);
     if (pc.rope.rot_dim > 0) {
         AppendArgs t{};
         t.n_heads = 2 * c.n_heads;          // q and k side by side
@@ -820,7 +820,7 @@ static upr_status run_extend(const upr_model* m, const typename Types::kv* emb, 
     UPR_LAUNCH("extend.init_ln1",
                launch_init_layernorm<T, TA>(emb + p.row0 * d, bf ? nullptr : g, a, R, d, m->layers[0].ln1_g,
                                             m->layers[0].ln1_b, c.ln_eps, nullptr, s));
-    const AttnArgs at = paged_attn_args(c, qkv, p.row0, o, bf ? ATTN_OUT_F16 : ATTN_OUT_STORAGE, false);
+    const AttnArgs at = paged_attn_args(c, pc.plan, qkv, p.row0, o, bf ? ATTN_OUT_F16 : ATTN_OUT_STORAGE, false);
     AppendArgs ap{};
     ap.n_heads = ap.n_kv_heads = c.n_heads;
     ap.D = D;
@@ -1291,7 +1291,7 @@ size_t upr_paged_cache_bytes(const upr_config* cfg, int64_t n_pages, int32_t pag
 // the tokens are looked at only if there are rows).
 static upr_status paged_plan(const upr_model* m, const upr_paged_cache* cache, const upr_segments* seg,
                              const char* name, const int32_t* rows_host, const upr_rope* rope, bool own,
-                             upr::RankPlan* p) {
+                             upr::RankPlan* p, upr::AttnArgs* plan) {
     if (!m) return fail(UPR_ERR_NULL, "model is NULL");
     upr_status st = upr::check_paged_cache(cache, false);
     int64_t rows = 0;
@@ -1303,29 +1303,33 @@ static upr_status paged_plan(const upr_model* m, const upr_paged_cache* cache, c
     upr::AttnArgs a{};
     a.n_heads = a.n_kv_heads = m->cfg.n_heads;
     a.D = m->cfg.head_dim;
-    a.k_self.p = own ? m : nullptr;
-    *p = upr::plan_paged(m->cfg, seg->num_users, seg->offsets_host,
-                         rows == 0 ? 0 : upr::paged_attn_workspace(upr::paged_dtype(m->cfg), a, seg, rows_host));
+    a.k_self.p = own ? m : nullptr;         // (only whether there are own keys)
+    const size_t bytes = rows == 0 ? 0 : upr::plan_paged_attn(upr::paged_dtype(m->cfg), &a, seg, rows_host);
+    *p = upr::plan_paged(m->cfg, seg->num_users, seg->offsets_host, bytes);
+    a.k_self.p = nullptr;
+    *plan = a;
     return UPR_OK;
 }
 
 static upr::PagedCall paged_call(const upr_model* m, const upr_paged_cache* cache, const int32_t* rows_host,
-                                 const upr_rope* rope) {
+                                 const upr_rope* rope, const upr::AttnArgs& plan) {
     return upr::PagedCall{cache, rows_host, upr::rope_args(rope),
-                          upr_paged_cache_bytes(&m->cfg, cache->n_pages, cache->page_rows) / m->cfg.n_layers};
+                          upr_paged_cache_bytes(&m->cfg, cache->n_pages, cache->page_rows) / m->cfg.n_layers, plan};
 }
 
 size_t upr_extend_workspace_bytes(const upr_model* m, const upr_paged_cache* cache, const upr_segments* fresh,
                                   const int32_t* rows_host) {
     upr::RankPlan p;
-    return paged_plan(m, cache, fresh, "fresh", rows_host, nullptr, false, &p) == UPR_OK ? p.bytes : 0;
+    upr::AttnArgs plan;
+    return paged_plan(m, cache, fresh, "fresh", rows_host, nullptr, false, &p, &plan) == UPR_OK ? p.bytes : 0;
 }
 
 upr_status upr_extend_user(const upr_model* m, const upr_paged_cache* cache, const void* emb,
                            const upr_segments* fresh, const int32_t* rows_host, const upr_rope* rope, void* ws,
                            size_t ws_bytes, void* stream) {
     upr::RankPlan p;
-    upr_status st = paged_plan(m, cache, fresh, "fresh", rows_host, rope, false, &p);
+    upr::AttnArgs plan;
+    upr_status st = paged_plan(m, cache, fresh, "fresh", rows_host, rope, false, &p, &plan);
     if (st != UPR_OK) return st;
     if (p.rows == 0) return ok();
     if (!emb) return fail(UPR_ERR_NULL, "emb is NULL");
@@ -1336,7 +1340,7 @@ upr_status upr_extend_user(const upr_model* m, const upr_paged_cache* cache, con
     arm_stop_hook();
     hipStream_t s = static_cast<hipStream_t>(stream);
     char* w = static_cast<char*>(ws);
-    const upr::PagedCall pc = paged_call(m, cache, rows_host, rope);
+    const upr::PagedCall pc = paged_call(m, cache, rows_host, rope, plan);
     st = bf16_family(m->cfg.dtype)
              ? upr::run_extend<upr::Bf16Types>(m, static_cast<const bf16*>(emb), fresh, pc, p, w, s)
              : upr::run_extend<upr::F32Types>(m, static_cast<const float*>(emb), fresh, pc, p, w, s);
@@ -1346,14 +1350,16 @@ upr_status upr_extend_user(const upr_model* m, const upr_paged_cache* cache, con
 size_t upr_rank_paged_workspace_bytes(const upr_model* m, const upr_paged_cache* cache, const upr_segments* cand,
                                       const int32_t* rows_host) {
     upr::RankPlan p;
-    return paged_plan(m, cache, cand, "cand", rows_host, nullptr, true, &p) == UPR_OK ? p.bytes : 0;
+    upr::AttnArgs plan;
+    return paged_plan(m, cache, cand, "cand", rows_host, nullptr, true, &p, &plan) == UPR_OK ? p.bytes : 0;
 }
 
 upr_status upr_rank_candidates_paged(const upr_model* m, const upr_paged_cache* cache, const int32_t* rows_host,
                                      const void* cand_emb, const upr_segments* cand, const upr_rope* rope,
                                      float* scores, void* ws, size_t ws_bytes, void* stream) {
     upr::RankPlan p;
-    upr_status st = paged_plan(m, cache, cand, "cand", rows_host, rope, true, &p);
+    upr::AttnArgs plan;
+    upr_status st = paged_plan(m, cache, cand, "cand", rows_host, rope, true, &p, &plan);
     if (st != UPR_OK) return st;
     if (p.rows == 0) return ok();
     if (!cand_emb) return fail(UPR_ERR_NULL, "cand_emb is NULL");
@@ -1365,7 +1371,7 @@ upr_status upr_rank_candidates_paged(const upr_model* m, const upr_paged_cache* 
     arm_stop_hook();
     hipStream_t s = static_cast<hipStream_t>(stream);
     char* w = static_cast<char*>(ws);
-    const upr::PagedCall pc = paged_call(m, cache, rows_host, rope);
+    const upr::PagedCall pc = paged_call(m, cache, rows_host, rope, plan);
     upr::RankOut out;
     out.scores = scores;
     st = bf16_family(m->cfg.dtype)

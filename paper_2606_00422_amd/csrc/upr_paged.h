@@ -57,10 +57,9 @@ struct AppendArgs {
     void* q_out;
     int64_t q_out_ld;
 };
-// Heads per thread for a call of `rows` rows, and the work items of `count`
-// rows of one user.
+// Heads per thread for a call of `rows` rows, and the rows of a work item.
 int append_batch(int dtype, const RopeArgs& rope, const AppendArgs& a, int64_t rows);
-int64_t append_items(int dtype, const RopeArgs& rope, const AppendArgs& a, int batch, int64_t count);
+int append_rows(int dtype, const RopeArgs& rope, const AppendArgs& a, int batch);
 hipError_t launch_append(int dtype, const RopeArgs& rope, const AppendArgs& a, int batch, const PagedPool& pool,
                          const PagedUsers& users, hipStream_t s);
 

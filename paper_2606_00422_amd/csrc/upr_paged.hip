@@ -154,24 +154,28 @@ static hipError_t each_launch(const upr_segments* seg, const int32_t* rows_host,
                               const Items& items, const Launch& launch) {
     constexpr int64_t kMaxItems = 1 << 23;      // of 256 threads
     const int32_t* const o = seg->offsets_host;
-    int32_t who[kPagedUsers];
+    struct Entry {
+        int32_t user, items;
+    };
+    Entry e[kPagedUsers];
     int64_t total = 0;
     int n = 0;
     auto flush = [&]() {
         if (longest_first)
-            std::sort(who, who + n, [&](int32_t x, int32_t y) {
-                return rows_host[x] != rows_host[y] ? rows_host[x] > rows_host[y] : x < y;
+            std::sort(e, e + n, [&](const Entry& x, const Entry& y) {
+                const int32_t a = rows_host[x.user], b = rows_host[y.user];
+                return a != b ? a > b : x.user < y.user;
             });
         PagedUsers u;
         u.n = n;
         u.item0[0] = 0;
         for (int i = 0; i < n; ++i) {
-            const int32_t w = who[i], c = o[w + 1] - o[w];
+            const int32_t w = e[i].user;
             u.user[i] = w;
             u.row0[i] = o[w];
-            u.count[i] = c;
+            u.count[i] = o[w + 1] - o[w];
             u.rows[i] = rows_host[w];
-            u.item0[i + 1] = u.item0[i] + (int32_t)items(c, rows_host[w]);
+            u.item0[i + 1] = u.item0[i] + e[i].items;
         }
         n = 0;
         total = 0;
@@ -183,10 +187,10 @@ static hipError_t each_launch(const upr_segments* seg, const int32_t* rows_host,
         const int64_t m = items(c, rows_host[w]);
         if (m > kMaxItems) return hipErrorInvalidConfiguration;
         if (n == kPagedUsers || (n > 0 && total + m > kMaxItems)) {
-            const hipError_t e = flush();
-            if (e != hipSuccess) return e;
+            const hipError_t st = flush();
+            if (st != hipSuccess) return st;
         }
-        who[n++] = w;
+        e[n++] = Entry{w, (int32_t)m};
         total += m;
     }
     return n > 0 ? flush() : hipSuccess;
@@ -195,8 +199,9 @@ static hipError_t each_launch(const upr_segments* seg, const int32_t* rows_host,
 hipError_t paged_append(int dtype, const RopeArgs& rope, const AppendArgs& a, const PagedPool& pool,
                         const upr_segments* seg, const int32_t* rows_host, hipStream_t s) {
     const int batch = append_batch(dtype, rope, a, (int64_t)seg->offsets_host[seg->num_users] - seg->offsets_host[0]);
+    const int per = append_rows(dtype, rope, a, batch);
     return each_launch(
-        seg, rows_host, false, [&](int32_t c, int32_t) { return append_items(dtype, rope, a, batch, c); },
+        seg, rows_host, false, [&](int32_t c, int32_t) { return (int64_t)((c + per - 1) / per); },
         [&](const PagedUsers& u) { return launch_append(dtype, rope, a, batch, pool, u, s); });
 }
 
@@ -277,7 +282,7 @@ static int attn_chunk(int dtype, const AttnArgs& a, const upr_segments* seg, con
 
 // Tile, parts and workspace of a call, from its lengths alone.  part_ml holds an
 // offset until the workspace is known.
-static size_t plan_attn(int dtype, AttnArgs* a, const upr_segments* seg, const int32_t* rows_host) {
+size_t plan_paged_attn(int dtype, AttnArgs* a, const upr_segments* seg, const int32_t* rows_host) {
     const int32_t* const o = seg->offsets_host;
     a->tile = attn_tile(dtype, *a, seg);
     a->chunk = attn_chunk(dtype, *a, seg, rows_host);
@@ -304,15 +309,9 @@ static size_t plan_attn(int dtype, AttnArgs* a, const upr_segments* seg, const i
     return sums + recs * 8;
 }
 
-size_t paged_attn_workspace(int dtype, const AttnArgs& args, const upr_segments* seg, const int32_t* rows_host) {
-    AttnArgs a = args;
-    return plan_attn(dtype, &a, seg, rows_host);
-}
-
-hipError_t paged_attn(int dtype, const AttnArgs& args, const PagedPool& pool, const upr_segments* seg,
+hipError_t paged_attn(int dtype, AttnArgs a, const PagedPool& pool, const upr_segments* seg,
                       const int32_t* rows_host, void* ws, hipStream_t s) {
-    AttnArgs a = args;
-    const bool join = plan_attn(dtype, &a, seg, rows_host) > 0;
+    const bool join = a.chunk > 0;
     if (join) {
         a.part_o = static_cast<float*>(ws);
         a.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) + reinterpret_cast<uintptr_t>(a.part_ml));
@@ -484,7 +483,8 @@ size_t upr_paged_attention_workspace_bytes(const upr_attn_shape* shape, const up
         check_paged_users(queries, "query", rows_host, cache->page_rows, cache->table_stride, shape->n_heads,
                           !options->k_self, &rows) != UPR_OK)
         return 0;
-    return paged_attn_workspace(shape->dtype, attn_args(*shape, *options), queries, rows_host);
+    AttnArgs a = attn_args(*shape, *options);
+    return plan_paged_attn(shape->dtype, &a, queries, rows_host);
 }
 
 upr_status upr_paged_attention(const upr_attn_shape* shape, const upr_paged_cache* cache,
@@ -510,7 +510,7 @@ upr_status upr_paged_attention(const upr_attn_shape* shape, const upr_paged_cach
     }
     if (st != UPR_OK) return st;
     AttnArgs a = attn_args(*shape, *options);
-    const size_t need = paged_attn_workspace(dt, a, queries, rows_host);
+    const size_t need = plan_paged_attn(dt, &a, queries, rows_host);
     if (need > 0) {
         if (!ws) return report_error(UPR_ERR_NULL, "workspace is NULL (%zu bytes needed)", need);
         if (ws_bytes < need)

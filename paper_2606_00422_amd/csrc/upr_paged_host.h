@@ -21,8 +21,10 @@ RopeArgs rope_args(const upr_rope* r);      // NULL: none
 // The launches of validated arguments (users of `seg`, cached rows rows_host).
 hipError_t paged_append(int dtype, const RopeArgs& rope, const AppendArgs& a, const PagedPool& pool,
                         const upr_segments* seg, const int32_t* rows_host, hipStream_t s);
-size_t paged_attn_workspace(int dtype, const AttnArgs& a, const upr_segments* seg, const int32_t* rows_host);
-hipError_t paged_attn(int dtype, const AttnArgs& a, const PagedPool& pool, const upr_segments* seg,
+// plan_paged_attn sets a's plan (tile, chunk, part_ml's offset) and returns the
+// workspace's bytes; paged_attn takes the planned arguments.
+size_t plan_paged_attn(int dtype, AttnArgs* a, const upr_segments* seg, const int32_t* rows_host);
+hipError_t paged_attn(int dtype, AttnArgs a, const PagedPool& pool, const upr_segments* seg,
                       const int32_t* rows_host, void* ws, hipStream_t s);
 
 }  // namespace upr

@@ -458,6 +458,11 @@ def _device() -> int:
     return torch.cuda.current_device()
 
 
+def _stream(stream, dev: int) -> int:
+    import torch
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream
+
+
 def _check_here(t, name, dev=None):
     import torch
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
@@ -561,7 +566,7 @@ def rope_apply(x, positions, rope: upr_rope, out=None, stream=None):
     if positions.dim() != 1 or positions.shape[0] != rows:
         raise ValueError("positions must be [rows]")
     status = load().upr_rope_apply(rope, _paged_dtype(x.dtype, "x"), heads, dim, px, ldx, positions.data_ptr(), rows,
-                                   po, ldo, current_stream() if stream is None else stream)
+                                   po, ldo, _stream(stream, dev))
     if status:
         _check(status)
     return out
@@ -601,11 +606,12 @@ class PagedCache:
         shape = self.data.shape
         return shape[-3], shape[-1], self.data.dtype
 
-    def view(self, users: int, layer=None) -> upr_paged_cache:
+    def view(self, users: int, layer=None, dev=None) -> upr_paged_cache:
         """The C struct, of one layer's plane or (None) of the whole pool."""
         data, tables = self.data, self.tables
-        if data.get_device() != _device():
-            raise ValueError(f"the cache is on {data.device}, the current device is cuda:{_device()}")
+        dev = _device() if dev is None else dev
+        if data.get_device() != dev:
+            raise ValueError(f"the cache is on {data.device}, the current device is cuda:{dev}")
         shape = data.shape
         held, width = tables.shape
         if held < users:
@@ -642,8 +648,8 @@ def paged_append(cache: PagedCache, off_host, rows_host, k, v, rope=None, q=None
         same = q is not None and _like(q_out, q)
         po, ldo = (q_out.data_ptr(), ldq) if same else _rows3(q_out, "q_out", dev, dt, n_heads, D, rows)
     shape = upr_attn_shape(_paged_dtype(dt, "data"), n_heads, H, D)
-    status = load().upr_paged_append(shape, cache.view(users, layer), seg, _host_rows(rows_host, users), rope, pk, ldk,
-                                     pv, ldv, pq, ldq, po, ldo, current_stream() if stream is None else stream)
+    status = load().upr_paged_append(shape, cache.view(users, layer, dev), seg, _host_rows(rows_host, users), rope, pk, ldk,
+                                     pv, ldv, pq, ldq, po, ldo, _stream(stream, dev))
     if status:
         _check(status)
 
@@ -698,9 +704,8 @@ def paged_attention(cache: PagedCache, off_host, rows_host, q, out=None, scale=N
         ws = paged_attention_workspace(cache, off_host, rows_host, n_heads, window, k_self is not None, stream)
     _check_flat(ws, "ws", dev, torch.uint8)
     shape = upr_attn_shape(_paged_dtype(dt, "data"), n_heads, H, D)
-    status = load().upr_paged_attention(shape, cache.view(users, layer), seg, _host_rows(rows_host, users), opt, pq, ldq,
-                                        po, ldo, ws.data_ptr(), ws.numel(),
-                                        current_stream() if stream is None else stream)
+    status = load().upr_paged_attention(shape, cache.view(users, layer, dev), seg, _host_rows(rows_host, users), opt, pq, ldq,
+                                        po, ldo, ws.data_ptr(), ws.numel(), _stream(stream, dev))
     if status:
         _check(status)
     return out
