@@ -237,6 +237,10 @@ __global__ __launch_bounds__(64 * RW * KW, RW > 1 && D < 128 ? (EX ? 3 : 4) : 2)
     constexpr int CR = D * (int)sizeof(T) / 16, RPL = 64 / CR;     // 16-byte chunks per row, rows per load
     constexpr int RPW = TS / NW, NI = RPW / RPL, NP = RPW > 16 ? RPW / 16 : 1;
     constexpr int TR = 16 * QG * RW;
+    // One buffer instead of two where two fill a CU's LDS with one workgroup and
+    // the matrix instructions, not the loads, take the time (fp32, head_dim 128:
+    // 4 x 500 rows over 1000, 8 heads, 133 -> 110 us).
+    constexpr bool kSingle = !kBf && D == 128;
     static_assert(RW == 1 || KW == 1, "a wave's rows or keys");
     static_assert(KS % SB == 0 && RPW % RPL == 0 && NI >= 1 && NI <= 8 && NP <= 4, "stage");
     __shared__ __attribute__((aligned(16))) T sK0[TS * D];
@@ -365,7 +369,7 @@ __global__ __launch_bounds__(64 * RW * KW, RW > 1 && D < 128 ? (EX ? 3 : 4) : 2)
     __builtin_amdgcn_sched_barrier(0);
     issue_loads(sK0, sV0, 0);
     fetch_pages(1);
-    if constexpr (RW == 1) {
+    if constexpr (RW == 1 && !kSingle) {
         issue_loads(sK1, sV1, 1);
         fetch_pages(2);
     }
@@ -608,37 +612,53 @@ __global__ __launch_bounds__(64 * RW * KW, RW > 1 && D < 128 ? (EX ? 3 : 4) : 2)
     };
 
     if constexpr (RW == 1) {
-        // A wave loads the very rows that it reads: no barriers.  Two stages are
-        // under way to LDS and one from there to registers while a block is
-        // computed.  (Stages past the last are loads of nothing: without
+        // A wave loads the very rows that it reads: no barriers.  Two stages (one,
+        // kSingle) are under way to LDS and one from there to registers while a
+        // block is computed.  (Stages past the last are loads of nothing: without
         // branches around them the compiler knows that the rows have landed.)
         static_assert(KS == SB, "one block per stage");
         // computes stage st (its fragments in cur), reads stage st + 1 from LDS
         // and loads stage st + 2 where st was
         auto stage = [&](T* cK, T* cV, const T* nK, const T* nV, const Frags& cur, Frags& next, int st)
             __attribute__((always_inline)) {
-            wait_lds();
-            issue_loads(cK, cV, st + 2);
-            fetch_pages(st + 3);
-            wait_loads<2 * NI>();
+            if constexpr (!kSingle) {
+                wait_lds();
+                issue_loads(cK, cV, st + 2);
+                fetch_pages(st + 3);
+                wait_loads<2 * NI>();
+            } else {
+                wait_loads<0>();
+            }
             __builtin_amdgcn_sched_barrier(0);
             read_ks(nK, kg * KS, next);
             read_vs(nV, kg * KS, next);
+            if constexpr (kSingle) {
+                wait_lds();
+                issue_loads(cK, cV, st + 2);
+                fetch_pages(st + 3);
+            }
             const int kabs = k0 + st * TS + kg * KS;
             if (kabs < k1 && kabs < wend && kabs + SB > wbeg) sub_block(cur, kabs, [] {});
         };
-        wait_loads<4 * NI>();           // the rows
-        wait_loads<2 * NI>();           // the first stage
+        if constexpr (!kSingle) wait_loads<4 * NI>();       // the rows
+        wait_loads<kSingle ? 0 : 2 * NI>();                 // the first stage
         Frags f0, f1;
         __builtin_amdgcn_sched_barrier(0);
         read_ks(sK0, kg * KS, f0);
         read_vs(sV0, kg * KS, f0);
+        if constexpr (kSingle) {
+            wait_lds();
+            issue_loads(sK0, sV0, 1);
+            fetch_pages(2);
+        }
+        T* const oK = kSingle ? sK0 : sK1;
+        T* const oV = kSingle ? sV0 : sV1;
         int st = 0;
         for (; st + 2 <= nst; st += 2) {
-            stage(sK0, sV0, sK1, sV1, f0, f1, st);
-            stage(sK1, sV1, sK0, sV0, f1, f0, st + 1);
+            stage(sK0, sV0, oK, oV, f0, f1, st);
+            stage(oK, oV, sK0, sV0, f1, f0, st + 1);
         }
-        if (st < nst) stage(sK0, sV0, sK1, sV1, f0, f1, st);
+        if (st < nst) stage(sK0, sV0, oK, oV, f0, f1, st);
         wait_lds();
         wait_loads<0>();
         __syncthreads();        // (the merge writes over other waves' rows)
@@ -691,10 +711,10 @@ __global__ __launch_bounds__(64 * RW * KW, RW > 1 && D < 128 ? (EX ? 3 : 4) : 2)
     if constexpr (KW > 1) {
         // one slot per wave but the first group's, as many per array as fit
         constexpr int kWords = QG * (EB * 4 + 2), kSlots = TS * D * (int)sizeof(T) / (kWords * 256);
-        static_assert(RW == 1 && kSlots >= 1 && 4 * kSlots >= KW - 1, "merge space");
+        static_assert(RW == 1 && kSlots >= 1 && (kSingle ? 2 : 4) * kSlots >= KW - 1, "merge space");
         auto slot = [&](int w) __attribute__((always_inline)) {
             const int i = (w - 1) / kSlots;
-            return reinterpret_cast<float*>(i == 0 ? sK0 : i == 1 ? sK1 : i == 2 ? sV0 : sV1) +
+            return reinterpret_cast<float*>(kSingle ? (i == 0 ? sK0 : sV0) : i == 0 ? sK0 : i == 1 ? sK1 : i == 2 ? sV0 : sV1) +
                    (w - 1) % kSlots * kWords * 64 + lane;
         };
         float* const x = slot(kg > 0 ? kg : 1);

@@ -247,7 +247,7 @@ static int attn_tile(int dtype, const AttnArgs& a, const upr_segments* seg) {
 // longest item alone (tk per key) or as the device (256 CUs; cached bytes at
 // 5.2 TB/s) takes for all of them, whichever is more.  Parts pay where the item
 // is the longer by more than the join's launch; a part is then an eighth of the
-// device's time.  Long calls of single rows of 128 values, whose workgroups have
+// device's time.  Long bf16 calls of single rows of 128 values, whose workgroups have
 // a CU's LDS to themselves, are cut as well until there are four per CU: nothing
 // else covers a workgroup's start there.  Measured, us, unsplit / split:
 // single rows, 8 heads of 64: one user over 1024 rows 9.3 / 9.6, 2048 13.3 /
@@ -273,7 +273,7 @@ static int attn_chunk(int dtype, const AttnArgs& a, const upr_segments* seg, con
     }
     const double bytes = seen * 2 * D * elem(dtype);
     const double device = std::max({keys * tk / 256, bytes / 5.2e6, 2.0});
-    const bool even = a.tile == 16 && D == 128 && device > 60 && items < 4 * 256;
+    const bool even = dtype == UPR_BF16 && a.tile == 16 && D == 128 && device > 60 && items < 4 * 256;
     if (longest * tk <= device + 4 && !even) return 0;
     double chunk = device / tk / 8;
     if (even) chunk = std::min(chunk, keys / (4 * 256));
