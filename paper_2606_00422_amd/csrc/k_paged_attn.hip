@@ -26,6 +26,22 @@
 // workspace.  A row whose result is not finite (a masked key's NaN or infinite
 // value times probability 0, or scores beyond the reference's range) is done
 // again by attn_row, which touches visible keys only.
+//
+// What bounds it (MI355X; us from graphs of the calls):
+//  * single rows: the cache's bytes.  64 rows over 512-16384 cached rows, 32/8
+//    heads of 128, 2.15 GB: 391 us, 5.5 TB/s (a 1 GB copy moves 4.8 to 5.2).
+//    One row over 1024 rows, 8 heads of 64: 8.0 us, of which 4.8 are the launch
+//    and the chain of loads to the first keys, the rest a CU's 62 B/ns.
+//  * 128-row tiles: vector issue and the matrix cores in turn.  4 x 2048 rows over
+//    up to 8192, 32/8 heads of 128: 478 to 490 us, 1.07 to 1.09 PFLOP/s (a matrix
+//    product of 8192^3 reaches 1.14); before fragments were read ahead 542.  At
+//    head_dim 64 a score costs as many vector instructions for half the products:
+//    64 x 2000 candidates over 1024 rows, 8 heads: 340 to 355 us, 760 to 790
+//    TFLOP/s, vector units 66% and matrix cores 37% busy.
+//  * 32-row tiles: 48 chunks of 1-96 rows, window 1024, bias, 8 heads of 64, 97 MB:
+//    30 us, workgroup starts beside 19 us of cache reads.
+//  * fp32: the fp32 matrix rate (154 TFLOP/s) at one to two waves per SIMD: 6
+//    chunks of 20-200 rows, cap, 4 heads of 64: 20 us with the join.
 #include <type_traits>
 
 #include "paged_dev.h"
@@ -342,9 +358,9 @@ __global__ __launch_bounds__(64 * RW * KW, RW > 1 && D < 128 ? (EX ? 3 : 4) : 2)
     frag qf[QG][ES];
     f32x4 o[QG][EB];            // bf16: e = 16 eb + 4g + r; fp32: e = EB (4g + r) + eb
     // row sums: the product of the probabilities with ones (the sum of all keys
-    // so far, in all four registers), or where those registers are short (128 for
-    // four waves per SIMD), and in fp32, of the lane's keys
-    constexpr bool kOnes = kBf && (RW == 1 || D == 128);
+    // so far, in all four registers), or where registers are short (128 for four
+    // waves per SIMD; bias and cap), and in fp32, of the lane's keys
+    constexpr bool kOnes = kBf && (RW == 1 || (D == 128 && !EX));
     typedef std::conditional_t<kOnes, f32x4, float> lsum;
     lsum l[QG];
     float negm[QG], slope2[QG];
@@ -546,8 +562,9 @@ __global__ __launch_bounds__(64 * RW * KW, RW > 1 && D < 128 ? (EX ? 3 : 4) : 2)
         if (__any(passed)) {
 #pragma unroll
             for (int qg = 0; qg < QG; ++qg) {
-                const float z = quad_max(top[qg]) * c;
-                const float nm = z + negm[qg] > kSlack ? -z : negm[qg];
+                // (the same test as above, of the row: the branch may be another's)
+                const float x = quad_max(top[qg]);
+                const float nm = fmaf(x, c, negm[qg]) > kSlack ? -(x * c) : negm[qg];
                 const float alpha = fast_exp2(nm - negm[qg]);
                 negm[qg] = nm;
                 l[qg] *= alpha;
