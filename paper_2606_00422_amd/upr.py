@@ -524,13 +524,19 @@ def _host_rows(rows_host, users):
     return _host_ptr(rows_host)
 
 
-def _stream_workspace(nbytes: int, stream):
-    """A workspace for a call on `stream` (None: the current one)."""
+def _new(shape, dtype, stream):
+    """A new tensor for a call on `stream` (None: the current one), from that
+    stream's memory: what the current stream has freed may still be in use."""
     import torch
-    ws = torch.empty(max(nbytes, 256), dtype=torch.uint8, device="cuda")
-    if stream is not None and stream != current_stream():
-        ws.record_stream(torch.cuda.ExternalStream(stream))
-    return ws
+    if stream is None or stream == current_stream():
+        return torch.empty(shape, dtype=dtype, device="cuda")
+    with torch.cuda.stream(torch.cuda.ExternalStream(stream)):
+        return torch.empty(shape, dtype=dtype, device="cuda")
+
+
+def _stream_workspace(nbytes: int, stream):
+    import torch
+    return _new(max(nbytes, 256), torch.uint8, stream)
 
 
 def rope(rot_dim: int, base: float = 10000.0, layout: str = "half", scaling: str = "none", factor: float = 1.0,
@@ -549,13 +555,13 @@ def rope(rot_dim: int, base: float = 10000.0, layout: str = "half", scaling: str
 
 def rope_apply(x, positions, rope: upr_rope, out=None, stream=None):
     """x [rows, heads, head_dim] rotated, row r at positions[r] (int32), into out
-    (a new tensor without one; x itself for in place)."""
+    (a new tensor without one, of the call's stream; x itself for in place)."""
     import torch
     dev = _device()
     px, ldx = _rows3(x, "x", dev)
     rows, heads, dim = x.shape
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        out = _new(x.shape, x.dtype, stream)
     if _like(out, x):
         po, ldo = out.data_ptr(), ldx
     else:
@@ -674,7 +680,7 @@ def paged_attention_workspace(cache: PagedCache, off_host, rows_host, n_heads: i
 def paged_attention(cache: PagedCache, off_host, rows_host, q, out=None, scale=None, softcap: float = 0.0,
                     window: int = 0, slopes=None, k_self=None, v_self=None, ws=None, layer: int = 0, stream=None):
     """upr_paged_attention on tensors: q and out [rows, heads, head_dim] (out: a
-    new tensor without one), slopes float32 [heads], k_self and v_self
+    new tensor of the call's stream without one), slopes float32 [heads], k_self and v_self
     [rows, kv_heads, head_dim] for ranking candidates.  scale: 1 /
     sqrt(head_dim) by default."""
     import torch
@@ -685,7 +691,7 @@ def paged_attention(cache: PagedCache, off_host, rows_host, q, out=None, scale=N
     pq, ldq = _rows3(q, "q", dev, dt, None, D, rows)
     n_heads = q.shape[1]
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = _new(q.shape, q.dtype, stream)
     po, ldo = (out.data_ptr(), ldq) if _like(out, q) else _rows3(out, "out", dev, dt, n_heads, D, rows)
     if slopes is not None:
         _check_flat(slopes, "slopes", dev, torch.float32)

@@ -346,6 +346,32 @@ def test_graphs_and_streams():
     assert torch.equal(got, want[1])
 
 
+def test_new_tensors_come_from_the_calls_stream():
+    """What the current stream has freed may still be in use there: a call on
+    another stream does not write to it."""
+    rng = np.random.default_rng(18)
+    rows = np.asarray([3000], np.int32)
+    pages = Pages(rng, "bf16", rows, 4, 64, 64)
+    q, _ = normal(rng, "bf16", 1, 4, 64)
+    x = torch.zeros((8192, 4, 64), dtype=torch.bfloat16, device="cuda")
+    at = torch.zeros(8192, dtype=torch.int32, device="cuda")
+    side = torch.cuda.Stream()
+    size = upr.paged_attention_workspace(pages.cache(), offsets([1]), rows, 4).numel()
+    assert size > 256
+    torch.cuda.synchronize()
+    freed = [torch.empty_like(x).data_ptr()]
+    out = upr.rope_apply(x, at, upr.rope(64), stream=side.cuda_stream)
+    assert out.data_ptr() not in freed
+    freed = [torch.empty(size, dtype=torch.uint8, device="cuda").data_ptr()]
+    ws = upr.paged_attention_workspace(pages.cache(), offsets([1]), rows, 4, stream=side.cuda_stream)
+    assert ws.data_ptr() not in freed
+    freed = [torch.empty_like(q).data_ptr()]
+    got = upr.paged_attention(pages.cache(), offsets([1]), rows, q, ws=ws, stream=side.cuda_stream)
+    assert got.data_ptr() not in freed
+    torch.cuda.synchronize()
+    assert torch.equal(got, upr.paged_attention(pages.cache(), offsets([1]), rows, q))
+
+
 def test_wrappers_refuse():
     rng = np.random.default_rng(16)
     pages = Pages(rng, "bf16", [20], 2, 64, 16)
