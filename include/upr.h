@@ -505,8 +505,9 @@ upr_status upr_rope_apply(const upr_rope* rope, int32_t dtype, int32_t heads, in
  * rotated at their positions when rope is given (NULL: as they are).  With q,
  * the queries of the same rows go to q_out likewise (rotated, or copied
  * without rope; q_out may be q with the same leading dimension, and must not
- * overlap k, v or the pages otherwise); q and q_out are both NULL or both given.  Only the new rows' places in the pages are
- * written; two new rows of one call must not share a place.  Allocates nothing. */
+ * overlap k, v or the pages otherwise); q and q_out are both NULL or both
+ * given.  Only the new rows' places in the pages are written; two new rows of
+ * one call must not share a place.  Allocates nothing. */
 upr_status upr_paged_append(const upr_attn_shape* shape, const upr_paged_cache* cache, const upr_segments* fresh,
                             const int32_t* rows_host, const upr_rope* rope, const void* k, int64_t k_ld,
                             const void* v, int64_t v_ld, const void* q, int64_t q_ld, void* q_out,

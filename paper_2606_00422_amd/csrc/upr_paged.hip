@@ -152,7 +152,9 @@ upr_status check_model_rope(const upr_rope* r, int head_dim) { return r ? check_
 template <typename Items, typename Launch>
 static hipError_t each_launch(const upr_segments* seg, const int32_t* rows_host, bool longest_first,
                               const Items& items, const Launch& launch) {
-    constexpr int64_t kMaxItems = 1 << 23;      // of 256 threads
+    // (of at most 256 threads; the largest user that the checks let through has
+    // 2^27 / 16 items, and for each of up to 1024 key/value heads a part of one)
+    constexpr int64_t kMaxItems = (1 << 23) + 1024;
     const int32_t* const o = seg->offsets_host;
     struct Entry {
         int32_t user, items;
@@ -185,7 +187,6 @@ static hipError_t each_launch(const upr_segments* seg, const int32_t* rows_host,
         const int32_t c = o[w + 1] - o[w];
         if (c == 0) continue;
         const int64_t m = items(c, rows_host[w]);
-        if (m > kMaxItems) return hipErrorInvalidConfiguration;
         if (n == kPagedUsers || (n > 0 && total + m > kMaxItems)) {
             const hipError_t st = flush();
             if (st != hipSuccess) return st;

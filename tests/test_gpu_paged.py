@@ -426,3 +426,20 @@ def test_offsets_past_32_bits():
         want, bound = attend(vv[a:b], K, K, np.arange(n - (b - a), n), "bf16")
         assert_close(got[a:b], want, bound, f"user {u}")
     del wide, data
+
+
+def test_rows_of_the_largest_call():
+    """The most rows that a call takes of one user, 2^27 with their heads, where
+    each head's last tile is part empty: without history a row gives its value."""
+    H, D = 33, 32
+    rows = (1 << 27) // H
+    x = torch.empty((rows, H, D), dtype=torch.float32, device="cuda")
+    x.view(-1).copy_(torch.arange(D * 1009, dtype=torch.float32, device="cuda").repeat(x.numel() // (D * 1009) + 1)[:x.numel()])
+    x.mul_(2.0 ** -15)
+    cache = upr.PagedCache(torch.zeros((1, 2, H, 16, D), dtype=torch.float32, device="cuda"),
+                           torch.zeros((1, 1), dtype=torch.int32, device="cuda"))
+    out = torch.full_like(x, float("nan"))
+    upr.paged_attention(cache, offsets([rows]), np.zeros(1, np.int32), x, out=out, k_self=x, v_self=x)
+    for i in range(0, rows, 1 << 18):
+        assert torch.equal(out[i:i + (1 << 18)], x[i:i + (1 << 18)]), i
+    del x, out
