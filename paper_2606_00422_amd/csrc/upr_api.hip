@@ -1333,6 +1333,7 @@ upr_status upr_extend_user(const upr_model* m, const upr_paged_cache* cache, con
     if (st != UPR_OK) return st;
     if (p.rows == 0) return ok();
     if (!emb) return fail(UPR_ERR_NULL, "emb is NULL");
+    if (reinterpret_cast<uintptr_t>(emb) % 16 != 0) return fail(UPR_ERR_LIMIT, "emb is not 16-byte aligned");
     st = upr::check_paged_cache(cache, true);
     if (st == UPR_OK) st = check_workspace(ws, ws_bytes, p.bytes);
     if (st != UPR_OK) return st;
@@ -1364,6 +1365,8 @@ upr_status upr_rank_candidates_paged(const upr_model* m, const upr_paged_cache* 
     if (p.rows == 0) return ok();
     if (!cand_emb) return fail(UPR_ERR_NULL, "cand_emb is NULL");
     if (!scores) return fail(UPR_ERR_NULL, "scores is NULL");
+    if (reinterpret_cast<uintptr_t>(cand_emb) % 16 != 0)
+        return fail(UPR_ERR_LIMIT, "cand_emb is not 16-byte aligned");
     st = upr::check_paged_cache(cache, true);
     if (st == UPR_OK) st = check_workspace(ws, ws_bytes, p.bytes);
     if (st != UPR_OK) return st;

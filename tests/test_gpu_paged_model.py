@@ -192,3 +192,10 @@ def test_extend_in_a_graph_and_model_refusals():
         model.extend(X[:1], off, grown, cache)
     with pytest.raises(TypeError):
         model.extend(X.float(), off, grown, cache)
+    odd = torch.empty(X.numel() + 1, dtype=X.dtype, device="cuda")[1:].view(X.shape)
+    scores = torch.empty(2, dtype=torch.float32, device="cuda")
+    for call in (lambda: model.extend(odd, off, grown, cache),
+                 lambda: model.rank_paged(cache, rows, odd, off, scores)):
+        with pytest.raises(upr.UprError) as e:
+            call()
+        assert e.value.status == upr.UPR_ERR_LIMIT
