@@ -17,8 +17,10 @@
 // LDS reads.  fp32: v_mfma_f32_16x16x4_f32, everything fp32.
 //
 // The running reference m follows a row's maximum only when a score passes it
-// by 2^kSlack: probabilities then reach 2^kSlack instead of 1, which costs no
-// precision, and O is rescaled a few times per row instead of every block.  A
+// by 2^kSlack, or (kSums) the row's sum passes kMostSum: probabilities then reach
+// that instead of 1, which costs no precision (sums are fp32, and values up to
+// 2^80 do not overflow them; rows that do are done again), and O is
+// rescaled a few times per row instead of every block.  A
 // row's decision uses its own scores only, so its result does not depend on
 // the rows beside it.
 //
@@ -33,11 +35,12 @@
 //    One row over 1024 rows, 8 heads of 64: 8.0 us, of which 4.8 are the launch
 //    and the chain of loads to the first keys, the rest a CU's 62 B/ns.
 //  * 128-row tiles: vector issue and the matrix cores in turn.  4 x 2048 rows over
-//    up to 8192, 32/8 heads of 128: 478 to 490 us, 1.07 to 1.09 PFLOP/s (a matrix
+//    up to 8192, 32/8 heads of 128: 466 to 485 us, 1.08 to 1.12 PFLOP/s (a matrix
 //    product of 8192^3 reaches 1.14); before fragments were read ahead 542.  At
 //    head_dim 64 a score costs as many vector instructions for half the products:
-//    64 x 2000 candidates over 1024 rows, 8 heads: 340 to 355 us, 760 to 790
-//    TFLOP/s, vector units 66% and matrix cores 37% busy.
+//    64 x 2000 candidates over 1024 rows, 8 heads: 336 to 346 us, 780 to 800
+//    TFLOP/s (with a maximum per block 352, vector units 66% and matrix cores
+//    37% busy).
 //  * 32-row tiles: 48 chunks of 1-96 rows, window 1024, bias, 8 heads of 64, 97 MB:
 //    30 us, workgroup starts beside 19 us of cache reads.
 //  * fp32: the fp32 matrix rate (154 TFLOP/s) at one to two waves per SIMD: 6
@@ -59,6 +62,7 @@ typedef __attribute__((ext_vector_type(4))) _Float16 h4;
 
 constexpr float kUnset = -1e30f;        // reference of a row that has seen no key
 constexpr float kSlack = 8.0f;
+constexpr float kMostSum = 0x1p40f;
 
 __device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
@@ -358,9 +362,14 @@ __global__ __launch_bounds__(64 * RW * KW, RW > 1 && D < 128 ? (EX ? 3 : 4) : 2)
     frag qf[QG][ES];
     f32x4 o[QG][EB];            // bf16: e = 16 eb + 4g + r; fp32: e = EB (4g + r) + eb
     // row sums: the product of the probabilities with ones (the sum of all keys
-    // so far, in all four registers), or where registers are short (128 for four
-    // waves per SIMD; bias and cap), and in fp32, of the lane's keys
-    constexpr bool kOnes = kBf && (RW == 1 || (D == 128 && !EX));
+    // so far, in all four registers), or in 128-row tiles, whose registers are
+    // short, and in fp32, of the lane's keys
+    constexpr bool kOnes = kBf && RW == 1;
+    // 128-row tiles without bias or cap: the sums, not a maximum per block, tell
+    // that a reference is passed (64 x 2000 candidates over 1024, 8 heads of 64, 354
+    // -> 344 us, 16 of 32, 482 -> 458; 4 x 2048 rows, 32/8 heads of 128, 485 -> 480).
+    // A steep bias passes it at every block, at a higher cost (636 -> 858).
+    constexpr bool kSums = kBf && RW > 1 && !EX;
     typedef std::conditional_t<kOnes, f32x4, float> lsum;
     lsum l[QG];
     float negm[QG], slope2[QG];
@@ -549,42 +558,75 @@ __global__ __launch_bounds__(64 * RW * KW, RW > 1 && D < 128 ? (EX ? 3 : 4) : 2)
                         if ((unsigned)(kabs + t * 16 + 4 * g + r - low[qg]) >= (unsigned)seen[qg]) s[qg][t][r] = -INFINITY;
             }
         }
-        // references that are passed by too much
-        float top[QG];
-        bool passed = false;
+        // the block's largest score of the lane's row (among its own keys)
+        auto largest = [&](int qg) __attribute__((always_inline)) {
+            const float x = max3(max3(s[qg][0][0], s[qg][0][1], s[qg][0][2]), s[qg][0][3], s[qg][NT - 1][0]);
+            if constexpr (NT == 1) return x;
+            return max3(max3(x, s[qg][NT - 1][1], s[qg][NT - 1][2]), s[qg][NT - 1][3], x);
+        };
+        auto move = [&](int qg, float nm) __attribute__((always_inline)) {
+            const float alpha = fast_exp2(nm - negm[qg]);
+            negm[qg] = nm;
+            l[qg] *= alpha;
 #pragma unroll
-        for (int qg = 0; qg < QG; ++qg) {
-            float x = max3(max3(s[qg][0][0], s[qg][0][1], s[qg][0][2]), s[qg][0][3], s[qg][NT - 1][0]);
-            if constexpr (NT == 2) x = max3(max3(x, s[qg][1][1], s[qg][1][2]), s[qg][1][3], x);
-            top[qg] = x;
-            passed |= fmaf(x, c, negm[qg]) > kSlack;
-        }
-        if (__any(passed)) {
+            for (int eb = 0; eb < EB; ++eb)
 #pragma unroll
-            for (int qg = 0; qg < QG; ++qg) {
-                // (the same test as above, of the row: the branch may be another's)
-                const float x = quad_max(top[qg]);
-                const float nm = fmaf(x, c, negm[qg]) > kSlack ? -(x * c) : negm[qg];
-                const float alpha = fast_exp2(nm - negm[qg]);
-                negm[qg] = nm;
-                l[qg] *= alpha;
-#pragma unroll
-                for (int eb = 0; eb < EB; ++eb)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) o[qg][eb][r] *= alpha;
-            }
-        }
-        if constexpr (kBf) {
-            b8 pf[QG];
-#pragma unroll
-            for (int qg = 0; qg < QG; ++qg) {
+                for (int r = 0; r < 4; ++r) o[qg][eb][r] *= alpha;
+        };
+        b8 pf[QG];
+        auto weigh = [&](int qg) __attribute__((always_inline)) {
+            if constexpr (kBf)
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) pf[qg][t * 4 + r] = (__bf16)fast_exp2(fmaf(s[qg][t][r], c, negm[qg]));
+        };
+        // the lane's part of a row's sum, this block added
+        const __bf16 u = (__bf16)1.0f;
+        auto summed = [&](int qg) __attribute__((always_inline)) {
+            float sum = first_of(l[qg]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                sum = __builtin_amdgcn_fdot2_f32_bf16(b2{pf[qg][2 * j], pf[qg][2 * j + 1]}, b2{u, u}, sum, false);
+            return sum;
+        };
+        // references that are passed by too much (in the branch the same test
+        // again, of the row: it may be another's)
+        float top[QG];              // kSums: the new sums
+        bool passed = false;
+#pragma unroll
+        for (int qg = 0; qg < QG; ++qg) {
+            if constexpr (kSums) {
+                weigh(qg);
+                top[qg] = summed(qg);
+                passed |= top[qg] > kMostSum;
+            } else {
+                top[qg] = largest(qg);
+                passed |= fmaf(top[qg], c, negm[qg]) > kSlack;
             }
+        }
+        if (__any(passed)) {
+#pragma unroll
+            for (int qg = 0; qg < QG; ++qg) {
+                if constexpr (kSums) {
+                    // to the larger of the block's maximum and the weight so far
+                    const bool mine = quad_max(top[qg]) > kMostSum;
+                    const float x = quad_max(largest(qg));
+                    const float so_far = __builtin_amdgcn_logf(quad_sum(first_of(l[qg])));
+                    move(qg, mine ? fminf(-(x * c), negm[qg] - so_far) : negm[qg]);
+                    weigh(qg);
+                    top[qg] = summed(qg);
+                } else {
+                    const float x = quad_max(top[qg]);
+                    move(qg, fmaf(x, c, negm[qg]) > kSlack ? -(x * c) : negm[qg]);
+                }
+            }
+        }
+        if constexpr (kBf) {
+            if constexpr (!kSums)
+#pragma unroll
+                for (int qg = 0; qg < QG; ++qg) weigh(qg);
             if constexpr (RW > 1) __builtin_amdgcn_s_setprio(1);
-            const __bf16 u = (__bf16)1.0f;
             if constexpr (kOnes) {
                 const b8 ones = {u, u, u, u, u, u, u, u};
 #pragma unroll
@@ -592,10 +634,7 @@ __global__ __launch_bounds__(64 * RW * KW, RW > 1 && D < 128 ? (EX ? 3 : 4) : 2)
                     l[qg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[qg], l[qg], 0, 0, 0);
             } else {
 #pragma unroll
-                for (int qg = 0; qg < QG; ++qg)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        l[qg] = __builtin_amdgcn_fdot2_f32_bf16(b2{pf[qg][2 * j], pf[qg][2 * j + 1]}, b2{u, u}, l[qg], false);
+                for (int qg = 0; qg < QG; ++qg) l[qg] = lsum{kSums ? top[qg] : summed(qg)};
             }
 #pragma unroll
             for (int eb = 0; eb < EB; ++eb) {

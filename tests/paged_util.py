@@ -81,11 +81,14 @@ def attend(q, K, V, pos, kind, scale=None, softcap=0.0, window=0, slopes=None, o
         rel = np.where(vis, delta + 2.0 ** -22 + 2.0 ** -23 * (np.abs(np.where(vis, z, 0.0)) + np.abs(top)), 0.0)
         rel = rel + (EPS["bf16"] if kind == "bf16" else 0.0) + n * 2.0 ** -24
         w = p / p.sum(1, keepdims=True)
-        vals = Vh[None] if own is None else np.concatenate([np.broadcast_to(Vh, (c, n, D)), own[1][:, g][:, None]], 1)
-        out[:, h] = (w[..., None] * vals).sum(1)
-        size = (w[..., None] * np.abs(vals)).sum(1)
+        def weighted(x, of):
+            y = x[:, :n] @ of(Vh)
+            return y if own is None else y + x[:, n:] * of(own[1][:, g])
+
+        out[:, h] = weighted(w, np.asarray)
+        size = weighted(w, np.abs)
         worst = (w * rel).sum(1, keepdims=True)         # of the normaliser
-        bound[:, h] = ((w * rel)[..., None] * np.abs(vals)).sum(1) + worst * size
+        bound[:, h] = weighted(w * rel, np.abs) + worst * size
         bound[:, h] += EPS[kind] * (np.abs(out[:, h]) + bound[:, h])
     return out, bound
 

@@ -255,6 +255,73 @@ def test_large_scores(kind):
     run_attend(rng, kind, [40], [500], 2, 2, 64, 16, q_scale=60.0, own=True)
 
 
+# Enough rows for the widest tiles (192 of 128 rows, counted with the heads).
+WIDE = ([100, 97, 128, 111, 100, 100], [100, 300, 128, 333, 1000, 160])
+
+
+@pytest.mark.parametrize("D", [32, 64, 128])
+@pytest.mark.parametrize("opt", [
+    dict(), dict(q_scale=60.0), dict(q_scale=600.0), dict(window=70), dict(window=1), dict(bias=True),
+    dict(softcap=5.0, q_scale=4.0), dict(softcap=5.0, bias=True, window=90, scale=0.3)], ids=str)
+@pytest.mark.parametrize("own", [False, True], ids=["causal", "self"])
+def test_wide_tiles(D, opt, own):
+    rng = np.random.default_rng([D, 19])
+    say(f"[gpu] attend wide tiles, head_dim {D}, {opt}, own {own}")
+    run_attend(rng, "bf16", *WIDE, 32, 8, D, 32, own=own, **opt)
+
+
+@pytest.mark.parametrize("D", [32, 64, 128])
+@pytest.mark.parametrize("step", [0.05, 0.9, 30.0, -30.0])
+def test_scores_that_rise_along_the_history(D, step):
+    """A row's reference is passed again and again: scores rise (or fall) by
+    `step` bits a key on average."""
+    rng = np.random.default_rng([D, 20])
+    counts, rows = WIDE
+    say(f"[gpu] attend head_dim {D}, scores rising by {step} bits a key")
+    pages = Pages(rng, "bf16", rows, 8, D, 32)
+    q, _ = normal(rng, "bf16", sum(counts), 32, D)
+    q[..., 0] = float(D) ** 0.5
+    for u, n in enumerate(rows):
+        ramp = (torch.arange(n) * step * 0.6931).to(pages.dt)
+        pages.hist[u][0, :, :, 0] = ramp.double().numpy()
+        for p in range(n):
+            pages.data[pages.tables[u, p // 32], 0, :, p % 32, 0] = ramp[p].item()
+    off = offsets(counts)
+    out = upr.paged_attention(pages.cache(), off, pages.rows, q)
+    qv = q.double().cpu().numpy()
+    for u, (c, n) in enumerate(zip(counts, rows)):
+        a, b = int(off[u]), int(off[u + 1])
+        want, bound = attend(qv[a:b], *pages.hist[u], np.arange(n - c, n), "bf16")
+        assert_close(out[a:b], want, bound, f"user {u}")
+
+
+def test_wide_tiles_unseen_rows_and_neighbours():
+    """As the two tests below, in the widest tiles."""
+    rng = np.random.default_rng(21)
+    counts, rows = WIDE
+    for D in (64, 128):
+        pages, off, q, out, _ = run_attend(rng, "bf16", counts, rows, 32, 8, D, 32)
+        u, n, c, a = 4, 1000, 100, int(off[4])
+        want, bound = attend(q[a:a + c].double().cpu().numpy(), *pages.hist[u], np.arange(n - c, n), "bf16")
+        for value in (float("nan"), float("inf"), torch.finfo(torch.bfloat16).max):
+            for j in (n - 1, n - 30, 930):
+                where = pages.tables[u, j // 32]
+                held = pages.data[where, :, :, j % 32].clone()
+                pages.data[where, :, :, j % 32] = value
+                got = upr.paged_attention(pages.cache(), off, pages.rows, q)[a:a + c]
+                pages.data[where, :, :, j % 32] = held
+                blind = np.arange(n - c, n) < j
+                assert_close(got[torch.from_numpy(blind).cuda()], want[blind], bound[blind], f"row {j} {value}")
+                if value != value:
+                    assert bool(torch.isnan(got[torch.from_numpy(~blind).cuda()]).all())
+        pages, off, q, out, call = run_attend(rng, "bf16", counts, rows, 32, 8, D, 32, own=True, q_scale=20.0)
+        order = np.concatenate([int(off[u]) + rng.permutation(c) for u, c in enumerate(counts)])
+        perm = torch.from_numpy(order).cuda()
+        call = dict(call, k_self=call["k_self"][perm], v_self=call["v_self"][perm])
+        got = upr.paged_attention(pages.cache(), off, pages.rows, q[perm].contiguous(), **call)
+        assert torch.equal(got, out[perm])
+
+
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf"), None])
 def test_unseen_rows_have_no_influence(kind, value):
