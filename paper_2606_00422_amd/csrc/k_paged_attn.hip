@@ -593,18 +593,20 @@ __global__ __launch_bounds__(64 * RW * KW, RW > 1 && D < 128 ? (EX ? 3 : 4) : 2)
         // references that are passed by too much (in the branch the same test
         // again, of the row: it may be another's)
         float top[QG];              // kSums: the new sums
+        unsigned most = 0;          // (sums are positive: as integers they need no quieting)
         bool passed = false;
 #pragma unroll
         for (int qg = 0; qg < QG; ++qg) {
             if constexpr (kSums) {
                 weigh(qg);
                 top[qg] = summed(qg);
-                passed |= top[qg] > kMostSum;
+                most = max(most, __float_as_uint(top[qg]));
             } else {
                 top[qg] = largest(qg);
                 passed |= fmaf(top[qg], c, negm[qg]) > kSlack;
             }
         }
+        if constexpr (kSums) passed = most > __float_as_uint(kMostSum);
         if (__any(passed)) {
 #pragma unroll
             for (int qg = 0; qg < QG; ++qg) {
